@@ -69,7 +69,7 @@ enum {
 };
 
 enum { RANS_MODE_DENSE = 0, RANS_MODE_CSR = 1 };
-enum { RANS_F32 = 0, RANS_F16 = 1 };
+enum { RANS_F32 = 0, RANS_F16 = 1, RANS_BF16 = 2 }; /* RANS_BF16: block codes, norm and matrix product only */
 
 /* The paper's statement of the problem: bit width Q (Eq. 6), coding precision
  * n (Eq. 2-4, called M here), reshape N x K (Eq. 5).  mode selects what is
@@ -195,6 +195,82 @@ typedef struct {
 int rans_search_workspace_bytes(uint64_t n_elems, uint32_t q_bits, size_t *ws_bytes);
 int rans_search_reshape(const uint8_t *d_sym, uint64_t n_elems, uint32_t q_bits,
                         rans_reshape_result *d_result, void *d_ws, size_t ws_bytes, void *stream);
+
+/* ---- Block codes: matrices of 8-bit floating-point numbers with a scale for each block of 128 ----
+ *
+ * The other 8-bit form of a feature tensor, the one that a matrix product takes as it is.  A coded matrix is
+ * rows x cols codes, row r at d_code + r * ld, and binary32 scales (RANS_SCALE_F32) or exponent bytes e, 2^(e - 127)
+ * (RANS_SCALE_E8M0; 255 is NaN).  RANS_BLOCK_ROW: columns 128 b .. 128 b + 127 of row r have the scale
+ * d_scale[r * ld_scale + b]; RANS_BLOCK_TILE: rows 128 a .. 128 a + 127 share d_scale[a * ld_scale + b].  The last block
+ * of a row and the last tile may be short.  A value is its code times its scale.  Formats: RANS_E4M3 (largest 448, no
+ * infinity, NaN 0x7f / 0xff), RANS_E5M2 (largest 57344, infinities 0x7c / 0xfc).
+ *
+ * These entry points propagate NaN and infinities as floating-point arithmetic does; there is no data-dependent error
+ * and nothing to read with rans_last_status().  ld and ld_scale may be anything from the row's length up to 2^32, rows and
+ * cols 0 to 2^30.  Codes whose rows start on 16 bytes (d_code aligned, ld a multiple of 16) and tensors whose rows do are
+ * faster; none is refused for its alignment beyond its element's.  Nothing outside the described rows and columns is read
+ * or written.  Work goes to the device of `stream`.  A workspace needs no initialisation, and calls that may run at the
+ * same time (two streams, two graphs) need one each. */
+enum { RANS_E4M3 = 0, RANS_E5M2 = 1 };
+enum { RANS_SCALE_F32 = 0, RANS_SCALE_E8M0 = 1 };
+enum { RANS_BLOCK_ROW = 0, RANS_BLOCK_TILE = 1 };
+typedef struct {
+  uint64_t rows, cols;
+  uint64_t ld;         /* codes from a row to the next, >= cols                          */
+  uint64_t ld_scale;   /* scales from a row of scales to the next, >= ceil(cols / 128)   */
+  uint32_t format;     /* RANS_E4M3 / RANS_E5M2                                          */
+  uint32_t scale_type; /* RANS_SCALE_*                                                   */
+  uint32_t block;      /* RANS_BLOCK_*                                                   */
+  uint32_t reserved;   /* 0                                                              */
+} rans_blocks;
+
+/* Tensor -> codes and scales.  d_x: out->rows x out->cols elements of in_dtype, ld_x elements from a row to the next; with
+ * transpose != 0 it is out->cols x out->rows and its transpose is coded (the operand of a product that runs along d_x's
+ * rows).  a = the largest finite |x| of a block, v = the format's largest number: s = max(a / v, 2^-126), or the least
+ * power of two >= 2^-126 with v s >= a; s = 1 for a = 0; code = x * (1 / s) rounded to the nearest, ties to even.  NaN
+ * gives NaN, an infinity gives NaN (E4M3) or itself (E5M2); the rest of its block is coded as if it were not there. */
+int rans_block_quantize(const void *d_x, uint64_t ld_x, uint32_t in_dtype, int transpose, uint8_t *d_code, void *d_scale,
+                        const rans_blocks *out, void *stream);
+
+/* Codes and scales -> tensor of out_dtype: the binary32 product, rounded once to the nearest, ties to even. */
+int rans_block_dequantize(const uint8_t *d_code, const void *d_scale, const rans_blocks *in, uint32_t out_dtype, void *d_x_out,
+                          uint64_t ld_x, void *stream);
+
+/* The residual's addition and the root-mean-square norm in front of a layer, its output coded:
+ *   h = x + residual rounded to dtype, rstd = 1 / sqrt(mean(h^2) + eps), y = h * rstd * weight (binary32),
+ * each row by itself.  x, residual, sum, y: rows x cols elements of dtype, ld_* elements from a row to the next; weight:
+ * cols elements of dtype or binary32.  d_res, d_weight (all ones) and each of the outputs d_sum (h), d_rstd (binary32, one
+ * a row, for rans_norm_backward), d_y (y rounded to dtype) and d_code / d_scale (y coded as `out` says, RANS_BLOCK_ROW)
+ * may be NULL.  Outputs may be an input's own memory (same pointer, same ld). */
+typedef struct {
+  uint64_t rows, cols;  /* cols >= 1 */
+  uint64_t ld_x, ld_res, ld_sum, ld_y;
+  uint32_t dtype, weight_dtype; /* RANS_F32 / F16 / BF16; the weight's is dtype or RANS_F32 */
+  float eps;                    /* >= 0 */
+  uint32_t reserved;            /* 0 */
+} rans_norm_params;
+int rans_norm_quantize(const void *d_x, const void *d_res, const void *d_weight, const rans_norm_params *p, void *d_sum,
+                       float *d_rstd, void *d_y, uint8_t *d_code, void *d_scale, const rans_blocks *out, void *stream);
+
+/* Its gradients.  d_dy: the gradient of y (rows ld_y apart; the coding is passed through), d_dsum: the gradient that comes
+ * to h from elsewhere (rows ld_res apart; NULL: none), d_sum: h (rows ld_sum apart), d_rstd: as the forward call left it.
+ *   d_dx (rows ld_x apart) = rstd * (dy w - xh * mean(dy w xh)) + dsum, xh = h * rstd: the gradient of x and of the residual;
+ *   d_dweight (cols binary32 numbers; NULL: not wanted) = sum over the rows of dy * xh, always added in the same order.
+ * d_dx may be d_dy's, d_dsum's or d_sum's own memory.  Workspace (only where d_dweight is given): rans_norm_workspace_bytes(). */
+int rans_norm_workspace_bytes(const rans_norm_params *p, size_t *ws_bytes);
+int rans_norm_backward(const void *d_dy, const void *d_dsum, const void *d_sum, const void *d_weight, const float *d_rstd,
+                       const rans_norm_params *p, void *d_dx, float *d_dweight, void *d_ws, size_t ws_bytes, void *stream);
+
+/* C = A B^T of two coded matrices with the same cols and the same scale_type; A has row blocks, B row blocks or tiles.
+ * d_c: a->rows x b->rows elements of out_dtype, ld_c elements from a row to the next; cols = 0 gives zeros.  The products of
+ * a block are added on the matrix cores, its sum times both scales (whose binary32 product is taken first) is added in
+ * binary32.  Results of 16 bits go through the 8-bit instructions, binary32 results through the bf16 ones, whose sums
+ * keep all of binary32 (the 8-bit ones cut off what is about 2^-13 below the largest of their products and less).
+ * Workspace: rans_matmul_workspace_bytes() (may be 0: then d_ws may be NULL). */
+int rans_matmul_workspace_bytes(const rans_blocks *a, const rans_blocks *b, size_t *ws_bytes);
+int rans_block_matmul(const uint8_t *d_a, const void *d_a_scale, const rans_blocks *a, const uint8_t *d_b,
+                      const void *d_b_scale, const rans_blocks *b, uint32_t out_dtype, void *d_c, uint64_t ld_c, void *d_ws,
+                      size_t ws_bytes, void *stream);
 
 /* Parse the fixed 128-byte header on the host.  h_bytes: at least 128 bytes.
  * RANS_ERR_CORRUPT if the fields are not a valid header. */

@@ -14,19 +14,24 @@ from __future__ import annotations
 import ctypes as C
 import os
 import subprocess
+import tempfile
 
 import torch
 
 _DIR = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_DIR)
 SO_PATH = os.path.join(_DIR, "librans_if.so")
-SRC_PATH = os.path.join(_DIR, "csrc", "rans_if.hip")
+SRC_PATHS = tuple(os.path.join(_DIR, "csrc", name) for name in ("rans_if.hip", "rans_blocks.hip"))
 INC_DIR = os.path.join(_ROOT, "include")
 
 OK, ERR_ARG, ERR_SHAPE, ERR_ALPHABET, ERR_CAPACITY, ERR_WORKSPACE, ERR_NONFINITE, ERR_CORRUPT, ERR_HIP = (
     0, -1, -2, -3, -4, -5, -6, -7, -8)
 MODE_DENSE, MODE_CSR = 0, 1
-F32, F16 = 0, 1
+F32, F16, BF16 = 0, 1, 2  # BF16: block codes, norm and matrix product only
+E4M3, E5M2 = 0, 1
+SCALE_F32, SCALE_E8M0 = 0, 1
+BLOCK_ROW, BLOCK_TILE = 0, 1
+BLOCK = 128  # columns (and rows of a tile) that share a scale
 
 HIPCC_FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-ffp-contract=off",
                "-fhip-fp32-correctly-rounded-divide-sqrt",
@@ -34,13 +39,20 @@ HIPCC_FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-ffp-contract=off"
 
 
 def build_library(verbose: bool = False) -> str:
-    """Compile csrc/rans_if.hip for gfx950 into librans_if.so (in-tree)."""
+    """Compile csrc/*.hip for gfx950, one compiler each at the same time, and link librans_if.so (in-tree)."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc, *HIPCC_FLAGS, "-I", INC_DIR, "-shared", "-fPIC", "-o", SO_PATH, SRC_PATH]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if verbose or res.returncode != 0:
-        print(res.stdout, res.stderr)
-    if res.returncode != 0:
+    with tempfile.TemporaryDirectory() as tmp:
+        objs = [os.path.join(tmp, os.path.basename(src) + ".o") for src in SRC_PATHS]
+        jobs = [subprocess.Popen([hipcc, *HIPCC_FLAGS, "-I", INC_DIR, "-fPIC", "-c", "-o", obj, src], text=True,
+                                 stdout=subprocess.PIPE, stderr=subprocess.PIPE) for src, obj in zip(SRC_PATHS, objs)]
+        done = [(j, *j.communicate()) for j in jobs]
+        if all(j.returncode == 0 for j, _, _ in done):
+            link = subprocess.run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", SO_PATH, *objs], capture_output=True, text=True)
+            done.append((link, link.stdout, link.stderr))
+    for res, out, err in done:
+        if verbose or res.returncode != 0:
+            print(out, err)
+    if any(res.returncode != 0 for res, _, _ in done):
         raise RuntimeError("hipcc failed building librans_if.so")
     return SO_PATH
 
@@ -71,12 +83,26 @@ class Header(C.Structure):
                 ("x_min", C.c_float), ("x_max", C.c_float)]
 
 
+class Blocks(C.Structure):
+    """Layout of a matrix of 8-bit codes with block scales (rans_blocks)."""
+    _fields_ = [("rows", C.c_uint64), ("cols", C.c_uint64), ("ld", C.c_uint64), ("ld_scale", C.c_uint64),
+                ("format", C.c_uint32), ("scale_type", C.c_uint32), ("block", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class NormParams(C.Structure):
+    _fields_ = [("rows", C.c_uint64), ("cols", C.c_uint64), ("ld_x", C.c_uint64), ("ld_res", C.c_uint64),
+                ("ld_sum", C.c_uint64), ("ld_y", C.c_uint64), ("dtype", C.c_uint32), ("weight_dtype", C.c_uint32),
+                ("eps", C.c_float), ("reserved", C.c_uint32)]
+
+
 NOALLOC_WS_BYTES = 32 << 20
 
 EXPORTS = ("rans_workspace_bytes", "rans_quantize", "rans_encode", "rans_decode", "rans_dequantize",
            "rans_compress", "rans_compress_noalloc", "rans_decompress", "rans_peek_header", "rans_last_status",
            "rans_search_workspace_bytes", "rans_search_reshape", "rans_selftest_divide",
            "rans_profile_enable", "rans_profile_reset", "rans_profile_read",
+           "rans_block_quantize", "rans_block_dequantize", "rans_norm_quantize", "rans_norm_workspace_bytes",
+           "rans_norm_backward", "rans_matmul_workspace_bytes", "rans_block_matmul",
            "rans_strerror", "rans_profile_kernel_name")
 
 _lib = None
@@ -104,6 +130,14 @@ def lib() -> C.CDLL:
         L.rans_search_workspace_bytes.argtypes = [u64, u32, C.POINTER(sz)]
         L.rans_search_reshape.argtypes = [vp, u64, u32, vp, vp, sz, vp]
         L.rans_selftest_divide.argtypes = [vp, u64, vp]
+        BP, NP, i32 = C.POINTER(Blocks), C.POINTER(NormParams), C.c_int
+        L.rans_block_quantize.argtypes = [vp, u64, u32, i32, vp, vp, BP, vp]
+        L.rans_block_dequantize.argtypes = [vp, vp, BP, u32, vp, u64, vp]
+        L.rans_norm_quantize.argtypes = [vp, vp, vp, NP, vp, vp, vp, vp, vp, BP, vp]
+        L.rans_norm_workspace_bytes.argtypes = [NP, C.POINTER(sz)]
+        L.rans_norm_backward.argtypes = [vp, vp, vp, vp, vp, NP, vp, vp, vp, sz, vp]
+        L.rans_matmul_workspace_bytes.argtypes = [BP, BP, C.POINTER(sz)]
+        L.rans_block_matmul.argtypes = [vp, vp, BP, vp, vp, BP, u32, vp, u64, vp, sz, vp]
         L.rans_strerror.argtypes = [C.c_int]
         L.rans_strerror.restype = C.c_char_p
         L.rans_profile_enable.argtypes = [u64, u32]
@@ -242,6 +276,155 @@ def _host_words(n: int) -> torch.Tensor:
     t = torch.empty(n, dtype=torch.int64, pin_memory=True)
     C.memset(t.data_ptr(), 0, 8 * n)
     return t
+
+
+# ------------------------------------------------------------------ block codes, norm, matrix product
+
+def make_blocks(rows, cols, ld=None, ld_scale=None, format=E4M3, scale_type=SCALE_F32, block=BLOCK_ROW) -> Blocks:
+    """ld, ld_scale: the lengths that BlockMatrix gives its memory, where not told."""
+    return Blocks(rows, cols, -(-cols // 16) * 16 if ld is None else ld, -(-cols // (4 * BLOCK)) * 4 if ld_scale is None else ld_scale,
+                  format, scale_type, block, 0)
+
+
+def make_norm_params(rows, cols, dtype, weight_dtype, eps, ld_x=None, ld_res=None, ld_sum=None, ld_y=None) -> NormParams:
+    return NormParams(rows, cols, *(cols if ld is None else ld for ld in (ld_x, ld_res, ld_sum, ld_y)), dtype, weight_dtype, eps, 0)
+
+
+def workspace(ws_bytes: int, device="cuda") -> torch.Tensor:
+    """ws_bytes bytes of device memory aligned as the entry points want it."""
+    t = torch.empty(ws_bytes + 256, dtype=torch.uint8, device=device)
+    off = (-t.data_ptr()) % 256
+    return t[off:off + ws_bytes]
+
+
+def _on(first, *more):
+    """The stream of the first tensor's device, None where a tensor is in host memory or on another device."""
+    dev = first.device
+    if dev.type != "cuda":
+        return None
+    for t in more:
+        if t is not None and t.device != dev:
+            return None
+    return C.c_void_p(torch.cuda.current_stream(dev).cuda_stream)
+
+
+def _holds(t, rows, cols, ld):
+    """Whether a tensor's memory reaches to the end of rows x cols elements that are ld apart; an absent one does."""
+    return t is None or not rows or not cols or (rows - 1) * ld + cols <= _reach(t)
+
+
+def _reach(t):
+    """Elements from a tensor's first one to the end of its storage's last one that it can see."""
+    n = 1
+    for size, stride in zip(t.shape, t.stride()):
+        if size == 0:
+            return 0
+        n += (size - 1) * stride
+    return n
+
+
+def _holds_blocks(code, scale, b):
+    return _holds(code, b.rows, b.cols, b.ld) and _holds(scale, -(-b.rows // BLOCK) if b.block == BLOCK_TILE else b.rows,
+                                                         -(-b.cols // BLOCK), b.ld_scale)
+
+
+def rans_block_quantize(d_x, ld_x, in_dtype, transpose, d_code, d_scale, out) -> int:
+    st = _on(d_x, d_code, d_scale)
+    if st is None or not _holds_blocks(d_code, d_scale, out) or not _holds(d_x, *((out.cols, out.rows) if transpose else (out.rows, out.cols)), ld_x):
+        return ERR_ARG
+    return lib().rans_block_quantize(_p(d_x), ld_x, in_dtype, transpose, _p(d_code), _p(d_scale), out, st)
+
+
+def rans_block_dequantize(d_code, d_scale, blocks, out_dtype, d_x_out, ld_x) -> int:
+    st = _on(d_x_out, d_code, d_scale)
+    if st is None or not _holds_blocks(d_code, d_scale, blocks) or not _holds(d_x_out, blocks.rows, blocks.cols, ld_x):
+        return ERR_ARG
+    return lib().rans_block_dequantize(_p(d_code), _p(d_scale), blocks, out_dtype, _p(d_x_out), ld_x, st)
+
+
+def rans_norm_quantize(d_x, d_res, d_weight, p, d_sum, d_rstd, d_y, d_code, d_scale, out) -> int:
+    st = _on(d_x, d_res, d_weight, d_sum, d_rstd, d_y, d_code, d_scale)
+    rows, cols = p.rows, p.cols
+    if st is None or not (_holds(d_x, rows, cols, p.ld_x) and _holds(d_res, rows, cols, p.ld_res) and _holds(d_sum, rows, cols, p.ld_sum)
+                          and _holds(d_y, rows, cols, p.ld_y) and _holds(d_weight, 1, cols, cols) and _holds(d_rstd, 1, rows, rows)
+                          and (d_code is None or (out is not None and _holds_blocks(d_code, d_scale, out)))):
+        return ERR_ARG
+    return lib().rans_norm_quantize(_p(d_x), _p(d_res), _p(d_weight), p, _p(d_sum), _p(d_rstd), _p(d_y), _p(d_code), _p(d_scale), out, st)
+
+
+def rans_norm_workspace_bytes(p: NormParams):
+    ws = C.c_size_t()
+    rc = lib().rans_norm_workspace_bytes(p, C.byref(ws))
+    return rc, ws.value
+
+
+def rans_norm_backward(d_dy, d_dsum, d_sum, d_weight, d_rstd, p, d_dx, d_dweight, d_ws) -> int:
+    st = _on(d_dy, d_dsum, d_sum, d_weight, d_rstd, d_dx, d_dweight, d_ws)
+    rows, cols = p.rows, p.cols
+    if st is None or not (_holds(d_dy, rows, cols, p.ld_y) and _holds(d_dsum, rows, cols, p.ld_res) and _holds(d_sum, rows, cols, p.ld_sum)
+                          and _holds(d_dx, rows, cols, p.ld_x) and _holds(d_weight, 1, cols, cols) and _holds(d_rstd, 1, rows, rows)
+                          and _holds(d_dweight, 1, cols, cols)):
+        return ERR_ARG
+    return lib().rans_norm_backward(_p(d_dy), _p(d_dsum), _p(d_sum), _p(d_weight), _p(d_rstd), p, _p(d_dx), _p(d_dweight), _p(d_ws),
+                                    0 if d_ws is None else d_ws.numel() * d_ws.element_size(), st)
+
+
+def rans_matmul_workspace_bytes(a: Blocks, b: Blocks):
+    ws = C.c_size_t()
+    rc = lib().rans_matmul_workspace_bytes(a, b, C.byref(ws))
+    return rc, ws.value
+
+
+def rans_block_matmul(d_a, d_a_scale, a, d_b, d_b_scale, b, out_dtype, d_c, ld_c, d_ws) -> int:
+    st = _on(d_c, d_a, d_a_scale, d_b, d_b_scale, d_ws)
+    if st is None or not (_holds_blocks(d_a, d_a_scale, a) and _holds_blocks(d_b, d_b_scale, b) and _holds(d_c, a.rows, b.rows, ld_c)):
+        return ERR_ARG
+    return lib().rans_block_matmul(_p(d_a), _p(d_a_scale), a, _p(d_b), _p(d_b_scale), b, out_dtype, _p(d_c), ld_c, _p(d_ws),
+                                   0 if d_ws is None else d_ws.numel() * d_ws.element_size(), st)
+
+
+class BlockMatrix:
+    """A matrix of 8-bit codes with block scales, and its memory: rows of codes start on 16 bytes."""
+
+    def __init__(self, rows, cols, format=E4M3, scale_type=SCALE_F32, block=BLOCK_ROW, device="cuda"):
+        self.layout = make_blocks(rows, cols, format=format, scale_type=scale_type, block=block)
+        self.code = torch.empty(rows, self.layout.ld, dtype=torch.uint8, device=device)
+        self.scale = torch.empty(-(-rows // BLOCK) if block == BLOCK_TILE else rows, self.layout.ld_scale,
+                                 dtype=torch.uint8 if scale_type == SCALE_E8M0 else torch.float32, device=device)
+
+    @staticmethod
+    def _check(rc):
+        if rc:
+            raise RansError(rc)
+
+    def quantize(self, x: torch.Tensor, transpose=False):
+        """Codes of a tensor [rows, cols] ([cols, rows] with `transpose`) whose last dimension is contiguous."""
+        self._check(rans_block_quantize(x, _ld(x), _dtype_code(x), transpose, self.code, self.scale, self.layout))
+        return self
+
+    def dequantize(self, out: torch.Tensor):
+        self._check(rans_block_dequantize(self.code, self.scale, self.layout, _dtype_code(out), out, _ld(out)))
+        return out
+
+    def matmul(self, b: "BlockMatrix", out: torch.Tensor, ws=None):
+        """out = self b^T; ws: rans_matmul_workspace_bytes() bytes, allocated where not given."""
+        if ws is None:
+            rc, size = rans_matmul_workspace_bytes(self.layout, b.layout)
+            self._check(rc)
+            ws = workspace(size, out.device) if size else None
+        self._check(rans_block_matmul(self.code, self.scale, self.layout, b.code, b.scale, b.layout, _dtype_code(out), out, _ld(out), ws))
+        return out
+
+
+def _dtype_code(t):
+    return {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}[t.dtype]
+
+
+def _ld(t):
+    """Elements from a row of a matrix to the next; its rows are contiguous."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise RansError(ERR_SHAPE)
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
 def rans_strerror(code: int) -> str:

@@ -1,0 +1,169 @@
+"""Block codes, norm and matrix product: struct layouts, workspace sizes and refusals.  CPU only: every call here is refused
+on the host before anything is launched, or has nothing to do."""
+import ctypes as C
+import os
+
+import pytest
+import torch
+
+from oracle import blocks as O
+from paper_2511_11664_amd import binding as B
+
+FAKE = 1 << 20  # an aligned address that nothing dereferences
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(B.SO_PATH):
+        B.build_library()
+    return B.lib()
+
+
+def blocks(rows=4, cols=256, **kw):
+    base = dict(ld=256, ld_scale=4, format=0, scale_type=0, block=0)
+    base.update(kw)
+    return B.make_blocks(rows, cols, **base)
+
+
+def test_struct_layouts_match_header():
+    assert C.sizeof(B.Blocks) == 48 and C.sizeof(B.NormParams) == 64
+
+
+def test_default_leading_dimensions():
+    b = B.make_blocks(3, 1000)
+    assert (b.ld, b.ld_scale) == (1008, 8)
+    m = B.BlockMatrix(300, 1000, scale_type=B.SCALE_E8M0, block=B.BLOCK_TILE, device="cpu")
+    assert m.code.shape == (300, 1008) and m.scale.shape == (3, 8) and m.scale.dtype == torch.uint8
+
+
+@pytest.mark.parametrize("change, code", [
+    (dict(ld=255), B.ERR_SHAPE), (dict(ld_scale=1), B.ERR_SHAPE), (dict(format=2), B.ERR_ARG), (dict(scale_type=2), B.ERR_ARG),
+    (dict(block=2), B.ERR_ARG), (dict(rows=(1 << 30) + 1), B.ERR_ARG), (dict(ld=(1 << 32) + 1), B.ERR_ARG)])
+def test_layouts_refused(lib, change, code):
+    b = blocks(**change)
+    assert lib.rans_block_quantize(FAKE, 256, B.F32, 0, FAKE, FAKE, b, None) == code
+    assert lib.rans_block_dequantize(FAKE, FAKE, b, B.F32, FAKE, 256, None) == code
+    assert lib.rans_block_matmul(FAKE, FAKE, b, FAKE, FAKE, blocks(), B.F32, FAKE, 4, None, 0, None) == code
+    size = C.c_size_t()
+    assert lib.rans_matmul_workspace_bytes(b, blocks(), C.byref(size)) == code
+
+
+def test_quantize_arguments_refused(lib):
+    b = blocks()
+    q = lib.rans_block_quantize
+    assert q(None, 256, B.F32, 0, FAKE, FAKE, b, None) == B.ERR_ARG
+    assert q(FAKE, 256, B.F32, 0, None, FAKE, b, None) == B.ERR_ARG
+    assert q(FAKE, 256, B.F32, 0, FAKE, None, b, None) == B.ERR_ARG
+    assert q(FAKE, 256, B.F32, 0, FAKE, FAKE, None, None) == B.ERR_ARG
+    assert q(FAKE, 256, 3, 0, FAKE, FAKE, b, None) == B.ERR_ARG
+    assert q(FAKE + 2, 256, B.F32, 0, FAKE, FAKE, b, None) == B.ERR_ARG       # misaligned element
+    assert q(FAKE, 256, B.F32, 0, FAKE, FAKE + 2, b, None) == B.ERR_ARG       # misaligned scale
+    assert q(FAKE, 255, B.F32, 0, FAKE, FAKE, b, None) == B.ERR_SHAPE
+    assert q(FAKE, 3, B.F32, 1, FAKE, FAKE, b, None) == B.ERR_SHAPE           # x is 256 x 4 where its transpose is coded
+    assert q(FAKE, (1 << 32) + 1, B.F32, 0, FAKE, FAKE, b, None) == B.ERR_ARG
+    assert q(None, 256, B.F32, 0, None, None, blocks(rows=0), None) == B.OK   # nothing to do
+    assert q(None, 256, B.F32, 0, None, None, blocks(cols=0), None) == B.OK
+    d = lib.rans_block_dequantize
+    assert d(FAKE, FAKE, b, B.BF16, FAKE + 1, 256, None) == B.ERR_ARG
+    assert d(FAKE, FAKE, b, B.BF16, None, 256, None) == B.ERR_ARG
+    assert d(FAKE, FAKE, b, 3, FAKE, 256, None) == B.ERR_ARG
+    assert d(FAKE, FAKE, b, B.BF16, FAKE, 200, None) == B.ERR_SHAPE
+    assert d(None, None, blocks(rows=0), B.BF16, None, 256, None) == B.OK
+
+
+def norm_params(**kw):
+    base = dict(rows=4, cols=256, dtype=B.BF16, weight_dtype=B.BF16, eps=1e-5)
+    base.update(kw)
+    return B.make_norm_params(**base)
+
+
+@pytest.mark.parametrize("change, code", [
+    (dict(cols=0, ld_x=1, ld_res=1, ld_sum=1, ld_y=1), B.ERR_ARG), (dict(dtype=3), B.ERR_ARG), (dict(weight_dtype=3), B.ERR_ARG),
+    (dict(eps=-1.0), B.ERR_ARG), (dict(eps=float("nan")), B.ERR_ARG), (dict(eps=float("inf")), B.ERR_ARG), (dict(ld_x=255), B.ERR_SHAPE),
+    (dict(ld_res=255), B.ERR_SHAPE), (dict(ld_sum=255), B.ERR_SHAPE), (dict(ld_y=255), B.ERR_SHAPE), (dict(rows=(1 << 30) + 1), B.ERR_ARG)])
+def test_norm_params_refused(lib, change, code):
+    p = norm_params(**change)
+    size = C.c_size_t()
+    assert lib.rans_norm_workspace_bytes(p, C.byref(size)) == code
+    assert lib.rans_norm_quantize(FAKE, None, None, p, None, None, FAKE, None, None, None, None) == code
+    assert lib.rans_norm_backward(FAKE, None, FAKE, None, FAKE, p, FAKE, None, None, 0, None) == code
+
+
+def test_norm_arguments_refused(lib):
+    p, b = norm_params(), blocks()
+    f = lib.rans_norm_quantize
+    assert f(None, None, None, p, None, None, FAKE, None, None, None, None) == B.ERR_ARG
+    assert f(FAKE, None, None, p, None, None, None, None, None, None, None) == B.ERR_ARG             # no output at all
+    assert f(FAKE, None, None, p, None, None, None, FAKE, FAKE, None, None) == B.ERR_ARG             # codes without their layout
+    assert f(FAKE, None, None, p, None, None, None, FAKE, FAKE, blocks(block=1), None) == B.ERR_ARG  # a tile spans rows
+    assert f(FAKE, None, None, p, None, None, None, FAKE, FAKE, blocks(rows=5), None) == B.ERR_SHAPE
+    assert f(FAKE, None, None, p, None, None, None, FAKE, FAKE, blocks(cols=128), None) == B.ERR_SHAPE
+    assert f(FAKE + 1, None, None, p, None, None, FAKE, None, None, None, None) == B.ERR_ARG
+    assert f(FAKE, None, FAKE + 1, p, None, None, FAKE, None, None, None, None) == B.ERR_ARG
+    assert f(FAKE, None, FAKE, norm_params(weight_dtype=B.F16), None, None, FAKE, None, None, None, None) == B.ERR_ARG
+    assert f(None, None, None, norm_params(rows=0), None, None, None, None, None, None, None) == B.OK
+    g = lib.rans_norm_backward
+    assert g(None, None, FAKE, None, FAKE, p, FAKE, None, None, 0, None) == B.ERR_ARG
+    assert g(FAKE, None, None, None, FAKE, p, FAKE, None, None, 0, None) == B.ERR_ARG
+    assert g(FAKE, None, FAKE, None, None, p, FAKE, None, None, 0, None) == B.ERR_ARG
+    assert g(FAKE, None, FAKE, None, FAKE, p, None, None, None, 0, None) == B.ERR_ARG
+    assert g(FAKE, None, FAKE, FAKE, FAKE, norm_params(weight_dtype=B.F16), FAKE, None, None, 0, None) == B.ERR_ARG
+    size = C.c_size_t()
+    assert lib.rans_norm_workspace_bytes(p, C.byref(size)) == B.OK and size.value >= 4 * 256 * 4
+    assert lib.rans_norm_workspace_bytes(p, None) == B.ERR_ARG
+    assert g(FAKE, None, FAKE, None, FAKE, p, FAKE, FAKE, None, size.value, None) == B.ERR_ARG
+    assert g(FAKE, None, FAKE, None, FAKE, p, FAKE, FAKE, FAKE + 16, size.value, None) == B.ERR_ARG
+    assert g(FAKE, None, FAKE, None, FAKE, p, FAKE, FAKE, FAKE, size.value - 1, None) == B.ERR_WORKSPACE
+
+
+def test_matmul_arguments_refused(lib):
+    a, b = blocks(), blocks(rows=8)
+    f = lib.rans_block_matmul
+    assert f(None, FAKE, a, FAKE, FAKE, b, B.BF16, FAKE, 8, None, 0, None) == B.ERR_ARG
+    assert f(FAKE, None, a, FAKE, FAKE, b, B.BF16, FAKE, 8, None, 0, None) == B.ERR_ARG
+    assert f(FAKE, FAKE, a, None, FAKE, b, B.BF16, FAKE, 8, None, 0, None) == B.ERR_ARG
+    assert f(FAKE, FAKE, a, FAKE, FAKE, b, B.BF16, None, 8, None, 0, None) == B.ERR_ARG
+    assert f(FAKE, FAKE, a, FAKE, FAKE, b, B.BF16, FAKE + 1, 8, None, 0, None) == B.ERR_ARG
+    assert f(FAKE, FAKE, a, FAKE, FAKE, b, 3, FAKE, 8, None, 0, None) == B.ERR_ARG
+    assert f(FAKE, FAKE, a, FAKE, FAKE, b, B.BF16, FAKE, 7, None, 0, None) == B.ERR_SHAPE
+    assert f(FAKE, FAKE, blocks(block=1), FAKE, FAKE, b, B.BF16, FAKE, 8, None, 0, None) == B.ERR_ARG      # A has row blocks
+    assert f(FAKE, FAKE, a, FAKE, FAKE, blocks(scale_type=1), B.BF16, FAKE, 8, None, 0, None) == B.ERR_ARG
+    assert f(FAKE, FAKE, a, FAKE, FAKE, blocks(cols=128), B.BF16, FAKE, 8, None, 0, None) == B.ERR_SHAPE
+    assert f(None, None, blocks(rows=0), None, None, b, B.BF16, None, 8, None, 0, None) in (B.ERR_ARG, B.OK)
+    size = C.c_size_t()
+    assert lib.rans_matmul_workspace_bytes(a, b, None) == B.ERR_ARG
+    assert lib.rans_matmul_workspace_bytes(a, b, C.byref(size)) == B.OK
+
+
+def test_binding_refuses_host_tensors_and_short_memory(lib):
+    x = torch.zeros(4, 256)
+    code, scale = torch.zeros(4, 256, dtype=torch.uint8), torch.zeros(4, 4)
+    b = blocks()
+    assert B.rans_block_quantize(x, 256, B.F32, False, code, scale, b) == B.ERR_ARG
+    assert B.rans_block_dequantize(code, scale, b, B.F32, x, 256) == B.ERR_ARG
+    assert B.rans_norm_quantize(x, None, None, norm_params(dtype=B.F32, weight_dtype=B.F32), None, None, x, None, None, None) == B.ERR_ARG
+    assert B.rans_norm_backward(x, None, x, None, x[0], norm_params(dtype=B.F32, weight_dtype=B.F32), x, None, None) == B.ERR_ARG
+    assert B.rans_block_matmul(code, scale, b, code, scale, b, B.F32, x, 256, None) == B.ERR_ARG
+    assert B._holds(x, 4, 256, 256) and not B._holds(x, 4, 256, 257) and not B._holds(x, 5, 1, 256) and B._holds(x[:, :7], 4, 7, 256)
+    assert not B._holds_blocks(code, scale, blocks(rows=5)) and B._holds_blocks(code, scale[:1], blocks(block=1))
+    with pytest.raises(B.RansError):
+        B._ld(x.t())
+
+
+@pytest.mark.parametrize("fmt, dt", [(0, torch.float8_e4m3fn), (1, torch.float8_e5m2)])
+def test_oracle_formats_agree_with_torch(fmt, dt):
+    c = torch.arange(256, dtype=torch.uint8)
+    assert torch.equal(torch.nan_to_num(O.decode8(c, fmt), nan=-1e9), torch.nan_to_num(c.view(dt).double(), nan=-1e9))
+    v = torch.randn(20000, generator=torch.Generator().manual_seed(0)) * torch.exp2(torch.randint(-12, 9, (20000,), generator=torch.Generator().manual_seed(1)))
+    v = v.clamp(-O.VMAX[fmt], O.VMAX[fmt])
+    assert torch.equal(O.round8(v.double(), fmt), v.to(dt).double())
+
+
+@pytest.mark.parametrize("fmt", (0, 1))
+def test_oracle_scales_are_the_least_power_of_two(fmt):
+    """v s >= a > v s / 2, at a = v 2^e and next to it."""
+    v = O.VMAX[fmt]
+    a = torch.tensor([v, v * 2 ** -30, v * 2 ** 20, 1.0, 1.7499999, 1.75, 1.7500001, 3.0]).float().repeat(2, 1)
+    for i in range(a.shape[1]):
+        s = O.block_scales(a[:1, i:i + 1], fmt, True, False).item()
+        assert v * s >= a[0, i].item() > v * s / 2

@@ -1,0 +1,239 @@
+"""The norm with the residual's addition and coded output, and its gradients, on the GPU against 64 bits.
+
+Tolerances, u = 2^-24 the half step of binary32.  rstd: the sum of K squares, added in chains of at most K / 64 + 16 links
+(eight a lane and step, six and some between lanes and waves) of positive terms, so its relative error is below
+(K / 64 + 18) u, half of that after the root, and 4 u for the mean, eps, the root and the quotient.  y = h rstd w: 3 u more."""
+import pytest
+import torch
+
+from oracle import blocks as O
+from paper_2511_11664_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+CODE = {torch.float32: B.F32, torch.float16: B.F16, torch.bfloat16: B.BF16}
+EPS = 1e-5
+SHAPES = [(1, 1), (3, 7), (2, 128), (5, 129), (4, 512), (3, 513), (2, 1000), (7, 2048), (2, 4096), (3, 4100), (2, 8192), (2, 8200), (1, 20000), (700, 96)]
+
+
+def half_step(v, dtype):
+    """Half a step of the type at v: eps / 2 of the value, or half the smallest subnormal number."""
+    f = torch.finfo(dtype)
+    return v.abs() * f.eps / 2 + f.smallest_normal * f.eps / 2
+
+
+def rstd_tolerance(cols):
+    return (cols / 128 + 13) * U
+
+
+def data(rows, cols, dtype, seed=0):
+    g = torch.Generator().manual_seed(rows * 100000 + cols + seed)
+    x, r = (torch.randn(rows, cols, generator=g).to(dtype) for _ in range(2))
+    x[:, cols // 3] *= 20
+    if rows > 2:
+        x[1], r[1] = 0, 0
+    w = (1 + 0.2 * torch.randn(cols, generator=g))
+    return x, r, w
+
+
+def params(rows, cols, dtype, wdtype, **ld):
+    return B.make_norm_params(rows, cols, CODE[dtype], CODE[wdtype], EPS, **ld)
+
+
+def pitched(t, ld, off=0):
+    """A copy of a matrix on the GPU with rows ld apart, its first element off elements into its memory."""
+    whole = torch.full((t.shape[0] * ld + off + 16,), 7.0, dtype=t.dtype, device="cuda")
+    v = whole.as_strided(t.shape, (ld, 1), off)
+    v.copy_(t)
+    return v
+
+
+def check_codes(y, tol, code, scale, fmt, e8m0):
+    """code s is y rounded to 8 bits, for y known up to tol: half a step of the format at the code, no code over the largest,
+    and the scale that belongs to the largest |y| of its block, up to the same tolerance (a power of two may then be either
+    of two neighbours)."""
+    rows, cols = y.shape
+    s = torch.exp2(scale.cpu().double() - 127) if e8m0 else scale.cpu().double()
+    for f in (1 - 1e-4, 1 + 1e-4) if e8m0 else ():
+        assert ((s <= O.block_scales((y * 1.0001).float(), fmt, True, False)) & (s >= O.block_scales((y * 0.9999).float(), fmt, True, False))).all()
+    b = torch.nn.functional.pad(y.abs(), (0, -cols % 128)).view(rows, -1, 128).amax(2)
+    if not e8m0:
+        assert (((s - b / O.VMAX[fmt]).abs() <= (tol.max() + 2 * U) * s) | (b == 0)).all()
+    each = O.spread(s, rows, cols, False)
+    v = O.decode8(code.cpu(), fmt)
+    step = 2.0 ** -(3, 2)[fmt] * torch.clamp(v.abs(), min=2.0 ** (-6, -14)[fmt])
+    assert ((v * each - y).abs() <= each * step / 2 + (tol + 3 * U) * y.abs()).all()
+
+
+@pytest.mark.parametrize("wide_weight", (False, True))
+@pytest.mark.parametrize("residual", (False, True))
+@pytest.mark.parametrize("dtype", tuple(CODE))
+def test_norm(dtype, residual, wide_weight):
+    for i, (rows, cols) in enumerate(SHAPES):
+        x, r, w = data(rows, cols, dtype)
+        w = w if wide_weight else w.to(dtype)
+        h, rstd, y = O.norm(x, r if residual else None, w, EPS, dtype)
+        tol = torch.full((rows, 1), rstd_tolerance(cols) + 3 * U, dtype=torch.float64)
+        fmt, e8m0, odd = i % 2, i // 2 % 2 == 1, i % 3 == 2
+        ld, off = (cols + 3, 1) if odd else (cols, 0)
+        xd, rd = pitched(x, ld, off), pitched(r, ld + 2, off) if residual else None
+        total, out = pitched(torch.zeros_like(x), ld, off), pitched(torch.zeros_like(x), ld + 1, off)
+        m = B.BlockMatrix(rows, cols, fmt, int(e8m0))
+        got_rstd = torch.zeros(rows, device="cuda")
+        p = params(rows, cols, dtype, w.dtype, ld_x=ld, ld_res=ld + 2, ld_sum=ld, ld_y=ld + 1)
+        assert B.rans_norm_quantize(xd, rd, w.cuda(), p, total, got_rstd, out, m.code, m.scale, m.layout) == 0
+        assert torch.equal(total.cpu().double(), h), (rows, cols)
+        assert ((got_rstd.cpu().double() - rstd).abs() <= rstd_tolerance(cols) * rstd).all(), (rows, cols)
+        assert ((out.cpu().double() - y).abs() <= tol * y.abs() * 1.01 + half_step(y, dtype)).all(), (rows, cols)
+        check_codes(y, tol, m.code[:, :cols], m.scale[:, :-(-cols // 128)], fmt, e8m0)
+
+
+@pytest.mark.parametrize("cols", (96, 4096, 8200, 20000))
+def test_norm_in_place_and_parts(cols):
+    """Sums in the residual's own memory, each output by itself, no weight."""
+    x, r, _ = data(5, cols, torch.bfloat16)
+    p = params(5, cols, torch.bfloat16, torch.bfloat16)
+    h, rstd, y = O.norm(x, r, None, EPS, torch.bfloat16)
+    ref = torch.empty(5, cols, dtype=torch.bfloat16, device="cuda")
+    assert B.rans_norm_quantize(x.cuda(), r.cuda(), None, p, None, None, ref, None, None, None) == 0
+    assert ((ref.cpu().double() - y).abs() <= (rstd_tolerance(cols) + 3 * U) * 1.01 * y.abs() + half_step(y, torch.bfloat16)).all()
+    for which in ("x", "res"):
+        xd, rd = x.cuda(), r.cuda()
+        total = xd if which == "x" else rd
+        out = torch.empty_like(ref)
+        assert B.rans_norm_quantize(xd, rd, None, p, total, None, out, None, None, None) == 0
+        assert torch.equal(total.cpu().double(), h) and torch.equal(out, ref)
+    xd = x.cuda()
+    assert B.rans_norm_quantize(xd, r.cuda(), None, p, None, None, xd, None, None, None) == 0  # y over x
+    assert torch.equal(xd, ref)
+    got = torch.zeros(5, device="cuda")
+    assert B.rans_norm_quantize(x.cuda(), r.cuda(), None, p, None, got, None, None, None, None) == 0
+    assert ((got.cpu().double() - rstd).abs() <= rstd_tolerance(cols) * rstd).all()
+    m = B.BlockMatrix(5, cols)
+    assert B.rans_norm_quantize(x.cuda(), r.cuda(), None, p, None, None, None, m.code, m.scale, m.layout) == 0
+    check_codes(y, torch.full((5, 1), rstd_tolerance(cols) + 3 * U, dtype=torch.float64), m.code[:, :cols], m.scale[:, :-(-cols // 128)], 0, False)
+
+
+def test_norm_special_values():
+    """A row of zeros, eps = 0 on it, NaN and infinity spoil their own row alone."""
+    x, r, w = data(6, 300, torch.float32)
+    x[2, 7], x[3, 8] = float("nan"), float("inf")
+    p = B.make_norm_params(6, 300, B.F32, B.F32, 0.0)
+    out = torch.empty(6, 300, device="cuda")
+    assert B.rans_norm_quantize(x.cuda(), r.cuda(), w.cuda(), p, None, None, out, None, None, None) == 0
+    want = O.norm(x, r, w, 0.0, torch.float32)[2]
+    got = out.cpu().double()
+    assert got[1].isnan().all() and got[2].isnan().all()          # 0 * inf; NaN
+    assert got[3, 8].isnan() and (got[3, :8] == 0).all()           # inf * 0; finite * 0
+    for i in (0, 4, 5):
+        assert ((got[i] - want[i]).abs() <= (rstd_tolerance(300) + 4 * U) * want[i].abs()).all()
+
+
+def bwd_data(rows, cols, dtype, wide_weight, seed=0):
+    x, r, w = data(rows, cols, dtype, seed)
+    g = torch.Generator().manual_seed(seed + 77)
+    dy = torch.randn(rows, cols, generator=g).to(dtype)
+    rstd = (1 / torch.sqrt((x.double() ** 2).mean(1) + EPS)).float()
+    return dy, r, x, w if wide_weight else w.to(dtype), rstd
+
+
+def check_backward(rows, cols, dtype, dy, dsum, h, w, rstd, dx, dw):
+    """dx: the row's sum of g xh in chains as above, relative to the sum of its magnitudes, then a few operations of one
+    rounding; dw: chains of at most rows links."""
+    want, want_w = O.norm_backward(dy, dsum, h, w, rstd)
+    g, xh = (dy.double() if w is None else dy.double() * w.double()), h.double() * rstd.double()[:, None]
+    mean_abs = (g * xh).abs().mean(1, keepdim=True)
+    r = rstd.double()[:, None]
+    tol = r * (4 * U * g.abs() + xh.abs() * mean_abs * (cols / 64 + 24) * U) + 2 * U * want.abs() + (0 if dsum is None else 2 * U * dsum.double().abs())
+    assert ((dx.cpu().double() - want).abs() <= tol * 1.01 + half_step(want, dtype)).all(), (rows, cols)
+    if dw is not None:
+        assert ((dw.cpu().double() - want_w).abs() <= (rows + 4) * U * (dy.double() * xh).abs().sum(0)).all(), (rows, cols)
+
+
+@pytest.mark.parametrize("wide_weight", (False, True))
+@pytest.mark.parametrize("dtype", tuple(CODE))
+def test_norm_backward(dtype, wide_weight):
+    for i, (rows, cols) in enumerate(SHAPES + [(1500, 200), (600, 9000)]):
+        dy, ds, h, w, rstd = bwd_data(rows, cols, dtype, wide_weight)
+        ds = None if i % 4 == 1 else ds
+        ld, off = (cols + 3, 1) if i % 3 == 2 else (cols, 0)
+        p = params(rows, cols, dtype, w.dtype, ld_x=ld, ld_res=ld + 2, ld_sum=ld, ld_y=ld + 1)
+        dx = pitched(torch.zeros_like(h), ld, off)
+        dw = torch.full((cols,), 3.0, device="cuda")
+        rc, size = B.rans_norm_workspace_bytes(p)
+        assert rc == 0
+        args = (pitched(dy, ld + 1, off), None if ds is None else pitched(ds, ld + 2, off), pitched(h, ld, off), w.cuda(), rstd.cuda(), p)
+        assert B.rans_norm_backward(*args, dx, dw, B.workspace(size)) == 0
+        check_backward(rows, cols, dtype, dy, ds, h, w, rstd, dx, dw)
+        dx2, dw2 = torch.zeros_like(dx).as_strided(dx.shape, dx.stride()) if ld == cols else pitched(torch.zeros_like(h), ld, off), torch.empty_like(dw)
+        assert B.rans_norm_backward(*args, dx2, dw2, B.workspace(size)) == 0
+        assert torch.equal(dx, dx2) and torch.equal(dw, dw2)  # the same order every time
+        dx3 = pitched(torch.zeros_like(h), ld, off)
+        assert B.rans_norm_backward(*args, dx3, None, None) == 0
+        assert torch.equal(dx, dx3)
+
+
+@pytest.mark.parametrize("cols", (96, 4096, 8200, 20000))
+@pytest.mark.parametrize("over", ("dy", "dsum", "h"))
+def test_norm_backward_in_place(cols, over):
+    dy, ds, h, w, rstd = bwd_data(9, cols, torch.float32, True)
+    p = params(9, cols, torch.float32, torch.float32)
+    t = dict(dy=dy.cuda(), dsum=ds.cuda(), h=h.cuda())
+    assert B.rans_norm_backward(t["dy"], t["dsum"], t["h"], w.cuda(), rstd.cuda(), p, t[over], None, None) == 0
+    check_backward(9, cols, torch.float32, dy, ds, h, w, rstd, t[over], None)
+
+
+def test_norm_backward_of_no_rows_and_no_weight():
+    p = params(0, 50, torch.float32, torch.float32)
+    dw = torch.ones(50, device="cuda")
+    e = torch.empty(0, 50, device="cuda")
+    assert B.rans_norm_backward(e, None, e, None, torch.empty(0, device="cuda"), p, e, dw, None) == 0
+    assert (dw == 0).all()
+    dy, ds, h, _, rstd = bwd_data(4, 333, torch.float16, False)
+    dx = torch.empty(4, 333, dtype=torch.float16, device="cuda")
+    assert B.rans_norm_backward(dy.cuda(), ds.cuda(), h.cuda(), None, rstd.cuda(), params(4, 333, torch.float16, torch.float16), dx, None, None) == 0
+    check_backward(4, 333, torch.float16, dy, ds, h, None, rstd, dx, None)
+
+
+def test_norm_gradient_against_differences():
+    """Central differences of the forward formula in 64 bits, step 1e-4: their error is below 1e-6 of the gradient's size."""
+    rows, cols = 2, 40
+    g = torch.Generator().manual_seed(5)
+    x, dy, ds, w = torch.randn(rows, cols, generator=g), torch.randn(rows, cols, generator=g), torch.randn(rows, cols, generator=g), 1 + 0.3 * torch.randn(cols, generator=g)
+
+    def loss(x_, w_):
+        y = x_ / torch.sqrt((x_ * x_).mean(1, keepdim=True) + EPS) * w_
+        return (y * dy.double()).sum() + (x_ * ds.double()).sum()
+
+    rstd = torch.empty(rows, device="cuda")
+    out = torch.empty(rows, cols, device="cuda")
+    p = params(rows, cols, torch.float32, torch.float32)
+    assert B.rans_norm_quantize(x.cuda(), None, w.cuda(), p, None, rstd, out, None, None, None) == 0
+    dx, dw = torch.empty_like(out), torch.empty(cols, device="cuda")
+    assert B.rans_norm_backward(dy.cuda(), ds.cuda(), x.cuda(), w.cuda(), rstd, p, dx, dw, B.workspace(B.rans_norm_workspace_bytes(p)[1])) == 0
+    e, scale = 1e-4, 1e-5
+    for i in range(rows):
+        for j in range(0, cols, 7):
+            d = torch.zeros(rows, cols, dtype=torch.float64)
+            d[i, j] = e
+            diff = (loss(x.double() + d, w.double()) - loss(x.double() - d, w.double())) / (2 * e)
+            assert abs(diff.item() - dx[i, j].item()) <= scale * dx.abs().max().item()
+    for j in range(0, cols, 7):
+        d = torch.zeros(cols, dtype=torch.float64)
+        d[j] = e
+        diff = (loss(x.double(), w.double() + d) - loss(x.double(), w.double() - d)) / (2 * e)
+        assert abs(diff.item() - dw[j].item()) <= scale * dw.abs().max().item()
+
+
+def test_norm_offsets_beyond_32_bits():
+    ld, cols = (1 << 31) + 8, 300
+    x, r, w = data(3, cols, torch.bfloat16)
+    xd = torch.empty(2 * ld + cols, dtype=torch.bfloat16, device="cuda").as_strided((3, cols), (ld, 1))
+    xd.copy_(x)
+    p = params(3, cols, torch.bfloat16, torch.bfloat16, ld_x=ld, ld_sum=ld)
+    out = torch.empty(3, cols, dtype=torch.bfloat16, device="cuda")
+    assert B.rans_norm_quantize(xd, r.cuda(), w.to(torch.bfloat16).cuda(), p, xd, None, out, None, None, None) == 0
+    h, _, y = O.norm(x, r, w.to(torch.bfloat16), EPS, torch.bfloat16)
+    assert torch.equal(xd.cpu().double(), h)
+    assert ((out.cpu().double() - y).abs() <= (rstd_tolerance(cols) + 3 * U) * 1.01 * y.abs() + half_step(y, torch.bfloat16)).all()
