@@ -21,7 +21,8 @@ import torch
 _DIR = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_DIR)
 SO_PATH = os.path.join(_DIR, "librans_if.so")
-SRC_PATHS = tuple(os.path.join(_DIR, "csrc", name) for name in ("rans_if.hip", "rans_blocks.hip"))
+SRC_PATHS = tuple(os.path.join(_DIR, "csrc", name) for name in ("rans_if.hip", "rans_blocks.hip", "rans_matmul_narrow.hip",
+                                                                    "rans_matmul_wide.hip"))
 INC_DIR = os.path.join(_ROOT, "include")
 
 OK, ERR_ARG, ERR_SHAPE, ERR_ALPHABET, ERR_CAPACITY, ERR_WORKSPACE, ERR_NONFINITE, ERR_CORRUPT, ERR_HIP = (

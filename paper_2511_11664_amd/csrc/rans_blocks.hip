@@ -1,7 +1,8 @@
 // rans_blocks.hip -- block codes, norm and matrix product: host side and extern "C" entry points
 //
-// A translation unit of its own beside the codec's (rans_if.hip); the kernels are in rans_blocks.h, rans_norm.h and
-// rans_matmul.h.  Compiled with the same flags: no contraction by the compiler, fused multiply-adds are written out.
+// A translation unit of its own beside the codec's (rans_if.hip); the kernels are in rans_blocks.h and
+// rans_norm.h, the product's in rans_matmul.h, which rans_matmul_narrow.hip and rans_matmul_wide.hip compile.  The same flags:
+// no contraction by the compiler, fused multiply-adds are written out.
 
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
@@ -16,7 +17,7 @@
 #include "rans_common.h"
 #include "rans_blocks.h"
 #include "rans_norm.h"
-#include "rans_matmul.h"
+#include "rans_matmul_launch.h"
 
 namespace {
 
@@ -356,24 +357,14 @@ int rans_block_matmul(const uint8_t *d_a, const void *d_a_scale, const rans_bloc
   if (!a->rows || !b->rows) return RANS_OK;
   const size_t eb = elem_bytes(out_dtype);
   if (!d_c || !aligned_to(d_c, eb)) return RANS_ERR_ARG;
-  const uint64_t tiles_m = (a->rows + kMmTile - 1) / kMmTile, tiles_n = (b->rows + kMmTile - 1) / kMmTile;
-  if (tiles_m * tiles_n > 1u << 23) return RANS_ERR_ARG;
   hipStream_t st = (hipStream_t)stream;
   const StreamDevice on(st);
   if (!on.ok) return RANS_ERR_HIP;
   MatmulArgs p{d_a, d_b, d_a_scale, d_b_scale, d_c, a->ld, b->ld, a->ld_scale, b->ld_scale, ld_c, (uint32_t)a->rows, (uint32_t)b->rows,
                (uint32_t)a->cols, a->scale_type == RANS_SCALE_E8M0, b->block == RANS_BLOCK_TILE, out_dtype,
-               aligned_to(d_c, 4 * eb) && ld_c % 4 == 0};
-  return by_bool(a->format == RANS_E5M2, [&](auto fa) {
-    return by_bool(b->format == RANS_E5M2, [&](auto fb) {
-      return by_bool(out_dtype == RANS_F32, [&](auto exact) -> int {
-        PROF_LAUNCH(KID_BLOCK_MATMUL, (k_block_matmul<decltype(fa)::value, decltype(fb)::value, decltype(exact)::value>),
-                    dim3((uint32_t)(tiles_m * tiles_n)), dim3(kWG), 0, st, p, (uint32_t)tiles_m);
-        LAUNCH_CHECK();
-        return RANS_OK;
-      });
-    });
-  });
+               aligned_to(d_c, 16) && ld_c * eb % 16 == 0 ? 2 : aligned_to(d_c, 4 * eb) && ld_c % 4 == 0};
+  const int fmt = (a->format == RANS_E5M2 ? 2 : 0) + (b->format == RANS_E5M2 ? 1 : 0);
+  return out_dtype == RANS_F32 ? launch_matmul_wide(p, fmt, st) : launch_matmul_narrow(p, fmt, st);
 }
 
 }  // extern "C"

@@ -6,6 +6,7 @@
 
 #include <cstddef>
 #include <cstdint>
+#include <atomic>
 #include <mutex>
 #include <vector>
 
@@ -23,14 +24,15 @@ enum KernelId {
   KID_NORMALIZE, KID_ENCODE, KID_CHUNK_SCAN, KID_GATHER, KID_DEC_PREPARE, KID_DECODE, KID_ROW_SCAN,
   KID_CSR_EXPAND, KID_DEQUANT, KID_RS_MASK, KID_RS_COUNT, KID_RS_COST,
   KID_ENCODE_FEED, KID_DECODE_LEAN, KID_BLOCK_QUANT, KID_BLOCK_QUANT_TILE, KID_BLOCK_DEQUANT, KID_NORM_QUANT, KID_NORM_BWD,
-  KID_NORM_DW, KID_BLOCK_MATMUL, KID_COUNT
+  KID_NORM_DW, KID_BLOCK_MATMUL, KID_BLOCK_MATMUL_FEW, KID_BLOCK_MATMUL_ANY,
+  KID_COUNT
 };
 inline const char *const kKernelNames[KID_COUNT] = {
     "k_minmax", "k_qinfo", "k_quant_hist", "k_scan_u32", "k_csr_compact", "k_csr_rows",
     "k_normalize", "k_encode", "k_chunk_scan", "k_gather", "k_dec_prepare", "k_decode", "k_row_part",
     "k_csr_to_dense", "k_dequant", "k_rs_mask", "k_rs_count", "k_rs_cost",
     "k_encode_feed", "k_decode_lean", "k_block_quant", "k_block_quant_tile", "k_block_dequant", "k_norm_quant", "k_norm_bwd",
-    "k_norm_dw", "k_block_matmul"};
+    "k_norm_dw", "k_block_matmul", "k_block_matmul_few", "k_block_matmul_any"};
 
 struct ProfRecord {
   int kid;
@@ -86,5 +88,18 @@ inline void prof_keep(const ProfRecord &r) {
   } while (0)
 
 inline bool aligned_to(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
+
+// Compute units of the current device (0 if the query fails); asked once per device.
+inline uint32_t compute_units() {
+  static std::atomic<int> cached[64];
+  int dev = -1;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 0;
+  int v = cached[dev].load(std::memory_order_relaxed);
+  if (v == 0) {
+    if (hipDeviceGetAttribute(&v, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || v <= 0) return 0;
+    cached[dev].store(v, std::memory_order_relaxed);
+  }
+  return (uint32_t)v;
+}
 
 #pragma GCC visibility pop

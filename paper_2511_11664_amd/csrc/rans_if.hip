@@ -56,19 +56,6 @@ inline uint32_t next_seq() {
   return v;
 }
 
-// Compute units of the current device (0 if the query fails); asked once per device.
-inline uint32_t compute_units() {
-  static std::atomic<int> cached[64];
-  int dev = -1;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 0;
-  int v = cached[dev].load(std::memory_order_relaxed);
-  if (v == 0) {
-    if (hipDeviceGetAttribute(&v, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || v <= 0) return 0;
-    cached[dev].store(v, std::memory_order_relaxed);
-  }
-  return (uint32_t)v;
-}
-
 constexpr uint32_t kDecWideGroupMinChunks = 192;
 // Decoding waves (64 streams) up to which the decoder takes its LEAN form, and the symbols of a stream from which: its
 // refill comes every 32 symbols, and its longer start has to pay (decompress calls with it over without it, median of 1 to

@@ -1,0 +1,73 @@
+// rans_matmul_pick.h -- which kernel a matrix product takes
+//
+// Part of the translation units rans_matmul_narrow.hip and rans_matmul_wide.hip; not a stand-alone header.
+#pragma once
+
+namespace {
+
+constexpr uint64_t kMmMaxTiles = 1u << 22;  // work-groups of a launch
+
+typedef MmTile<2, 4, 8, 4, 2> MmLarge;   // 256 x 256, eight waves
+typedef MmTile<2, 4, 4, 2, 2> MmMedium;  // 128 x 128, eight waves
+typedef MmTile<2, 2, 4, 4, 2> MmWide;    // 128 x 128, four waves: widened operands, and operands of any alignment
+typedef MmTile<2, 2, 2, 2, 4> MmSmall;   // 64 x 64, four waves, four stages
+
+template <typename TILE> uint64_t mm_tiles(const MatmulArgs &p) { return ((p.m + TILE::bm - 1) / TILE::bm) * (uint64_t)((p.n + TILE::bn - 1) / TILE::bn); }
+
+template <typename TILE, int FA, int FB, int SCALE, bool EXACT> int launch_tiles(const MatmulArgs &p, hipStream_t st) {
+  const uint64_t tiles_m = (p.m + TILE::bm - 1) / TILE::bm, tiles_n = (p.n + TILE::bn - 1) / TILE::bn;
+  if (tiles_m * tiles_n > kMmMaxTiles) return RANS_ERR_ARG;
+  PROF_LAUNCH(KID_BLOCK_MATMUL, (k_block_matmul<TILE, FA, FB, SCALE, EXACT>), dim3((uint32_t)(tiles_m * tiles_n)), dim3(TILE::threads), 0, st, p,
+              (uint32_t)tiles_m, (uint32_t)tiles_n);
+  LAUNCH_CHECK();
+  return RANS_OK;
+}
+template <typename TILE, int FA, int FB, int SCALE, bool EXACT> int launch_any(const MatmulArgs &p, hipStream_t st) {
+  const uint64_t tiles_m = (p.m + TILE::bm - 1) / TILE::bm, tiles_n = (p.n + TILE::bn - 1) / TILE::bn;
+  if (tiles_m * tiles_n > kMmMaxTiles) return RANS_ERR_ARG;
+  PROF_LAUNCH(KID_BLOCK_MATMUL_ANY, (k_block_matmul_any<TILE, FA, FB, SCALE, EXACT>), dim3((uint32_t)(tiles_m * tiles_n)), dim3(TILE::threads), 0, st, p,
+              (uint32_t)tiles_m, (uint32_t)tiles_n);
+  LAUNCH_CHECK();
+  return RANS_OK;
+}
+template <int MT, int W, int AHEAD, int FA, int FB, int SCALE, bool EXACT> int launch_few(const MatmulArgs &p, hipStream_t st) {
+  PROF_LAUNCH(KID_BLOCK_MATMUL_FEW, (k_block_matmul_few<FA, FB, SCALE, EXACT, MT, W, AHEAD>), dim3((p.n + 15) / 16), dim3(W * 64), 0, st, p);
+  LAUNCH_CHECK();
+  return RANS_OK;
+}
+
+// Rounds of work-groups times what a round takes, us a block: `alone` with one work-group on a compute unit, `both` with two
+// (K = 4096, 256 units; 48 to 1024 rows of A, 1024 to 12288 of B).
+inline double mm_cost(uint64_t tiles, uint32_t units, double alone, double both) {
+  const uint64_t slots = both > 0 ? 2ull * units : units, whole = tiles / slots, rest = tiles % slots;
+  const double full = both > 0 ? both : alone;
+  return whole * full + (rest == 0 ? 0 : rest <= units ? alone : full);
+}
+inline double mm_cost_large(const MatmulArgs &p, uint32_t units) { return mm_cost(mm_tiles<MmLarge>(p), units, 1.6, 0); }
+inline double mm_cost_medium(const MatmulArgs &p, uint32_t units) { return mm_cost(mm_tiles<MmMedium>(p), units, 0.64, 1.1); }
+inline double mm_cost_small(const MatmulArgs &p, uint32_t units) { return mm_cost(mm_tiles<MmSmall>(p), units, 0.36, 0.5); }
+
+// Few rows of A: the kernel for them takes about 2.6 us and what B, and A once for every 16 rows of B, take at 7.9 MB a us;
+// `tiles` is what the tile kernel would take for a block.  1 / 16 / 32 rows, K = 4096, us, few rows over 64 x 64 tiles:
+// 4096 rows of B 4.4 / 6.5 / 9.4 over 12, 12288 rows of B 9.6 / 15.3 / 24.7 over 13.
+inline bool mm_few(const MatmulArgs &p, double tiles) {
+  if (p.m > 32 || p.n > kMmMaxTiles * 16) return false;
+  const double bytes = (double)p.n * p.k * (1 + p.m / 16.0), nb = (p.k + kBlk - 1) / kBlk;
+  return 2.6 + bytes / 7.9e6 < 1 + tiles * nb;
+}
+inline bool mm_fetch_fits(const MatmulArgs &p) {
+  return aligned_to(p.a, 16) && aligned_to(p.b, 16) && p.lda % 16 == 0 && p.ldb % 16 == 0 && p.lda <= kMmMaxLd && p.ldb <= kMmMaxLd;
+}
+
+template <typename F> int by_format(int fmt, F f) {
+  typedef std::integral_constant<int, 0> E4;
+  typedef std::integral_constant<int, 1> E5;
+  return fmt & 2 ? (fmt & 1 ? f(E5{}, E5{}) : f(E5{}, E4{})) : (fmt & 1 ? f(E4{}, E5{}) : f(E4{}, E4{}));
+}
+template <typename F> int by_scale(const MatmulArgs &p, F f) {
+  if (p.e8m0) return f(std::integral_constant<int, MM_E8M0>{});
+  if (p.b_tile) return f(std::integral_constant<int, MM_F32_TILE>{});
+  return f(std::integral_constant<int, MM_F32_ROW>{});
+}
+
+}  // namespace
