@@ -298,24 +298,34 @@ def workspace(ws_bytes: int, device="cuda") -> torch.Tensor:
     return t[off:off + ws_bytes]
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # the current stream's handle without a Stream object
+
+
 def _on(first, *more):
-    """The stream of the first tensor's device, None where a tensor is in host memory or on another device."""
-    dev = first.device
-    if dev.type != "cuda":
+    """The current stream's handle on the first tensor's device, None where a tensor is in host memory or on another device."""
+    dev = first.get_device()
+    if dev < 0:
         return None
     for t in more:
-        if t is not None and t.device != dev:
+        if t is not None and t.get_device() != dev:
             return None
-    return C.c_void_p(torch.cuda.current_stream(dev).cuda_stream)
+    return _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream(dev).cuda_stream
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
 
 
 def _holds(t, rows, cols, ld):
     """Whether a tensor's memory reaches to the end of rows x cols elements that are ld apart; an absent one does."""
-    return t is None or not rows or not cols or (rows - 1) * ld + cols <= _reach(t)
+    if t is None or not rows or not cols:
+        return True
+    need = (rows - 1) * ld + cols
+    return need <= t.numel() or need <= _reach(t)
 
 
 def _reach(t):
-    """Elements from a tensor's first one to the end of its storage's last one that it can see."""
+    """Elements from a tensor's first one to the last one that it can see."""
     n = 1
     for size, stride in zip(t.shape, t.stride()):
         if size == 0:
@@ -325,22 +335,22 @@ def _reach(t):
 
 
 def _holds_blocks(code, scale, b):
-    return _holds(code, b.rows, b.cols, b.ld) and _holds(scale, -(-b.rows // BLOCK) if b.block == BLOCK_TILE else b.rows,
-                                                         -(-b.cols // BLOCK), b.ld_scale)
+    rows, cols = b.rows, b.cols
+    return _holds(code, rows, cols, b.ld) and _holds(scale, -(-rows // BLOCK) if b.block else rows, -(-cols // BLOCK), b.ld_scale)
 
 
 def rans_block_quantize(d_x, ld_x, in_dtype, transpose, d_code, d_scale, out) -> int:
     st = _on(d_x, d_code, d_scale)
     if st is None or not _holds_blocks(d_code, d_scale, out) or not _holds(d_x, *((out.cols, out.rows) if transpose else (out.rows, out.cols)), ld_x):
         return ERR_ARG
-    return lib().rans_block_quantize(_p(d_x), ld_x, in_dtype, transpose, _p(d_code), _p(d_scale), out, st)
+    return lib().rans_block_quantize(_at(d_x), ld_x, in_dtype, transpose, _at(d_code), _at(d_scale), out, st)
 
 
 def rans_block_dequantize(d_code, d_scale, blocks, out_dtype, d_x_out, ld_x) -> int:
     st = _on(d_x_out, d_code, d_scale)
     if st is None or not _holds_blocks(d_code, d_scale, blocks) or not _holds(d_x_out, blocks.rows, blocks.cols, ld_x):
         return ERR_ARG
-    return lib().rans_block_dequantize(_p(d_code), _p(d_scale), blocks, out_dtype, _p(d_x_out), ld_x, st)
+    return lib().rans_block_dequantize(_at(d_code), _at(d_scale), blocks, out_dtype, _at(d_x_out), ld_x, st)
 
 
 def rans_norm_quantize(d_x, d_res, d_weight, p, d_sum, d_rstd, d_y, d_code, d_scale, out) -> int:
@@ -350,7 +360,7 @@ def rans_norm_quantize(d_x, d_res, d_weight, p, d_sum, d_rstd, d_y, d_code, d_sc
                           and _holds(d_y, rows, cols, p.ld_y) and _holds(d_weight, 1, cols, cols) and _holds(d_rstd, 1, rows, rows)
                           and (d_code is None or (out is not None and _holds_blocks(d_code, d_scale, out)))):
         return ERR_ARG
-    return lib().rans_norm_quantize(_p(d_x), _p(d_res), _p(d_weight), p, _p(d_sum), _p(d_rstd), _p(d_y), _p(d_code), _p(d_scale), out, st)
+    return lib().rans_norm_quantize(_at(d_x), _at(d_res), _at(d_weight), p, _at(d_sum), _at(d_rstd), _at(d_y), _at(d_code), _at(d_scale), out, st)
 
 
 def rans_norm_workspace_bytes(p: NormParams):
@@ -366,7 +376,7 @@ def rans_norm_backward(d_dy, d_dsum, d_sum, d_weight, d_rstd, p, d_dx, d_dweight
                           and _holds(d_dx, rows, cols, p.ld_x) and _holds(d_weight, 1, cols, cols) and _holds(d_rstd, 1, rows, rows)
                           and _holds(d_dweight, 1, cols, cols)):
         return ERR_ARG
-    return lib().rans_norm_backward(_p(d_dy), _p(d_dsum), _p(d_sum), _p(d_weight), _p(d_rstd), p, _p(d_dx), _p(d_dweight), _p(d_ws),
+    return lib().rans_norm_backward(_at(d_dy), _at(d_dsum), _at(d_sum), _at(d_weight), _at(d_rstd), p, _at(d_dx), _at(d_dweight), _at(d_ws),
                                     0 if d_ws is None else d_ws.numel() * d_ws.element_size(), st)
 
 
@@ -380,7 +390,7 @@ def rans_block_matmul(d_a, d_a_scale, a, d_b, d_b_scale, b, out_dtype, d_c, ld_c
     st = _on(d_c, d_a, d_a_scale, d_b, d_b_scale, d_ws)
     if st is None or not (_holds_blocks(d_a, d_a_scale, a) and _holds_blocks(d_b, d_b_scale, b) and _holds(d_c, a.rows, b.rows, ld_c)):
         return ERR_ARG
-    return lib().rans_block_matmul(_p(d_a), _p(d_a_scale), a, _p(d_b), _p(d_b_scale), b, out_dtype, _p(d_c), ld_c, _p(d_ws),
+    return lib().rans_block_matmul(_at(d_a), _at(d_a_scale), a, _at(d_b), _at(d_b_scale), b, out_dtype, _at(d_c), ld_c, _at(d_ws),
                                    0 if d_ws is None else d_ws.numel() * d_ws.element_size(), st)
 
 

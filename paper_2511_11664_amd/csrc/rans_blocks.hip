@@ -183,22 +183,35 @@ int check_norm(const rans_norm_params *p) {
   return RANS_OK;
 }
 
-constexpr uint32_t kNormSliceRows = 1u << 22;   // rows of a launch
-constexpr uint32_t kNormDwMaxParts = 512;       // work-groups of the gradient's kernel, and rows of partial sums
+constexpr uint32_t kNormSliceRows = 1u << 21;  // rows of a launch
 
-uint32_t norm_parts(const rans_norm_params &p) { return (uint32_t)(p.rows < kNormDwMaxParts ? p.rows : kNormDwMaxParts); }
+// The work-group that a row takes: f(threads, eights a thread); 0 eights: any length.
+template <int NT, int NV, typename F> int with_row(F f) { return f(std::integral_constant<int, NT>{}, std::integral_constant<int, NV>{}); }
 
-// The work-group that a row of `cols` elements takes: f(threads, eights a thread); 0 eights: any length.
-template <typename F> int by_row_length(uint64_t cols, F f) {
-  typedef std::integral_constant<int, 64> N64;
-  typedef std::integral_constant<int, 256> N256;
-#define CASE(NT, NV) f(N##NT{}, std::integral_constant<int, NV>{})
-  if (cols <= 64 * 8) return CASE(64, 1);
-  if (cols <= 256 * 8) return CASE(256, 1);
-  if (cols <= 256 * 8 * 2) return CASE(256, 2);
-  if (cols <= 256 * 8 * 4) return CASE(256, 4);
-  return CASE(256, 0);
-#undef CASE
+// Forward.  Few rows are quicker with more threads on each, many with more in flight for each thread: 4096 columns, 512 threads
+// over 256: 1 row 2.96 / 3.45 us, 512 rows 5.1 / 5.4, 16384 rows 84.7 / 83.4.
+template <typename F> int by_row_forward(const rans_norm_params &p, F f) {
+  const bool many = p.rows >= 4096;
+  if (p.cols <= 64 * 8) return with_row<64, 1>(f);
+  if (p.cols <= 256 * 8) return with_row<256, 1>(f);
+  if (p.cols <= 512 * 8) return many ? with_row<256, 2>(f) : with_row<512, 1>(f);
+  if (p.cols <= 1024 * 8) return many ? with_row<512, 2>(f) : with_row<1024, 1>(f);
+  return with_row<512, 0>(f);
+}
+
+// Backward, and its work-groups, which are the rows of partial sums too: one or two on a compute unit, since the next row's
+// loads are under way anyway and each partial row is written and read again.  16384 x 4096 with 256 / 512 of them 88.8 /
+// 95.6 us; 16384 x 2048 (256 threads each) 59.7 / 45.6; 395 x 5120 (1024 threads) 8.8, with one for every row 12.5.
+template <typename F> int by_row_backward(const rans_norm_params &p, F f) {
+  if (p.cols <= 64 * 8) return with_row<64, 1>(f);
+  if (p.cols <= 256 * 8) return with_row<256, 1>(f);
+  if (p.cols <= 512 * 8) return with_row<512, 1>(f);
+  if (p.cols <= 1024 * 8) return with_row<1024, 1>(f);
+  return with_row<512, 0>(f);
+}
+uint32_t norm_parts(const rans_norm_params &p) {
+  const uint32_t most = p.cols <= 64 * 8 ? 2048 : p.cols <= 256 * 8 ? 512 : 256;
+  return (uint32_t)(p.rows < most ? p.rows : most);
 }
 
 }  // namespace
@@ -243,7 +256,7 @@ int rans_norm_quantize(const void *d_x, const void *d_res, const void *d_weight,
       if (!decltype(same_tag)::value && p->weight_dtype != RANS_F32) return (int)RANS_ERR_ARG;
       return by_bool(d_code && out->scale_type == RANS_SCALE_E8M0, [&](auto e8m0_tag) {
         constexpr bool E8M0 = decltype(e8m0_tag)::value;
-        return by_row_length(p->cols, [&](auto nt_tag, auto nv_tag) -> int {
+        return by_row_forward(*p, [&](auto nt_tag, auto nv_tag) -> int {
           constexpr int NT = decltype(nt_tag)::value, NV = decltype(nv_tag)::value;
           for (uint64_t r = 0; r < p->rows; r += kNormSliceRows) {
             const uint32_t g = (uint32_t)(p->rows - r < kNormSliceRows ? p->rows - r : kNormSliceRows);
@@ -298,7 +311,7 @@ int rans_norm_backward(const void *d_dy, const void *d_dsum, const void *d_sum, 
       typedef decltype(elem) T;
       return by_bool(p->weight_dtype == p->dtype, [&](auto same_tag) {
         typedef typename std::conditional<decltype(same_tag)::value, T, float>::type W;
-        return by_row_length(p->cols, [&](auto nt_tag, auto nv_tag) -> int {
+        return by_row_backward(*p, [&](auto nt_tag, auto nv_tag) -> int {
           constexpr int NT = decltype(nt_tag)::value, NV = decltype(nv_tag)::value;
           PROF_LAUNCH(KID_NORM_BWD, (k_norm_bwd<T, W, NT, NV>), dim3(g), dim3(NT), 0, st, a);
           LAUNCH_CHECK();
@@ -309,7 +322,7 @@ int rans_norm_backward(const void *d_dy, const void *d_dsum, const void *d_sum, 
     if (rc) return rc;
   }
   if (d_dweight) {
-    PROF_LAUNCH(KID_NORM_DW, k_norm_dw, dim3((uint32_t)((p->cols + 63) / 64)), dim3(kWG), 0, st, (const float *)d_ws, g, (uint32_t)p->cols,
+    PROF_LAUNCH(KID_NORM_DW, k_norm_dw, dim3((uint32_t)((p->cols + 31) / 32)), dim3(kDwWG), 0, st, (const float *)d_ws, g, (uint32_t)p->cols,
                 d_dweight);
     LAUNCH_CHECK();
   }

@@ -30,11 +30,6 @@ template <int NT> __device__ inline float group_sum(float v, float *s) {
   return r;
 }
 
-template <typename W> __device__ inline f32x8 load_weight8(const W *w, uint32_t c, uint32_t n, bool vec) {
-  if (!w) return (f32x8){1, 1, 1, 1, 1, 1, 1, 1};
-  return load8(w, c, n, vec);
-}
-
 struct NormFwd {
   const void *x, *res, *weight;
   void *sum, *y;
@@ -48,52 +43,32 @@ struct NormFwd {
 };
 
 // A row per work-group of NT threads, NV times eight neighbouring elements a thread (NV = 0: any length, h read again).
+// Everything a thread needs from memory is requested before the row's sum, the weight too.
 template <typename T, typename W, bool E8M0, int NT, int NV>
 __global__ __launch_bounds__(NT) void k_norm_quant(NormFwd a, uint64_t row0) {
+  typedef typename Vec8<T>::type V;
   __shared__ float s_sum[NT / 64];
   const uint64_t row = row0 + blockIdx.x;
   const uint32_t t = threadIdx.x, n = a.cols;
   const T *x = (const T *)a.x + row * a.ld_x;
   const T *res = a.res ? (const T *)a.res + row * a.ld_res : nullptr;
   T *sum = a.sum ? (T *)a.sum + row * a.ld_sum : nullptr;
-  constexpr int NR = NV ? NV : 1;
-  f32x8 h[NR];
-  float acc = 0;
-  auto take = [&](uint32_t c) {
-    f32x8 v = load8(x, c, n, a.vec);
+  float acc = 0, rstd = 0;
+  auto add = [&](V v, V r) {
+    f32x8 h = float8_of(v);
     if (res) {
-      const f32x8 r = load8(res, c, n, a.vec);
 #pragma unroll
-      for (int i = 0; i < 8; i++) v[i] = (float)(T)(v[i] + r[i]);
+      for (int i = 0; i < 8; i++) h[i] = (float)(T)(h[i] + (float)r[i]);
     }
-    return v;
+    return h;
   };
-  if (NV) {
+  auto square = [&](f32x8 h) {
 #pragma unroll
-    for (int k = 0; k < NR; k++) {
-      const uint32_t c = (k * NT + t) * 8;
-      h[k] = c < n ? take(c) : (f32x8){0, 0, 0, 0, 0, 0, 0, 0};
-    }
-#pragma unroll
-    for (int k = 0; k < NR; k++) {
-      const uint32_t c = (k * NT + t) * 8;
-      if (sum && c < n) store8(sum, c, n, a.vec, h[k]);
-#pragma unroll
-      for (int i = 0; i < 8; i++) acc = __builtin_fmaf(h[k][i], h[k][i], acc);
-    }
-  } else {
-    for (uint32_t c = t * 8; c < n; c += NT * 8) {
-      const f32x8 v = take(c);
-      if (sum) store8(sum, c, n, a.vec, v);
-#pragma unroll
-      for (int i = 0; i < 8; i++) acc = __builtin_fmaf(v[i], v[i], acc);
-    }
-  }
-  const float rstd = 1.0f / sqrtf(group_sum<NT>(acc, s_sum) * a.inv_cols + a.eps);
-  if (a.rstd && t == 0) a.rstd[row] = rstd;
-  auto give = [&](uint32_t c, f32x8 v) {
+    for (int i = 0; i < 8; i++) acc = __builtin_fmaf(h[i], h[i], acc);
+  };
+  auto weight8 = [&](uint32_t c) { return a.weight ? load8((const W *)a.weight, c, n, a.vec_w) : (f32x8){1, 1, 1, 1, 1, 1, 1, 1}; };
+  auto give = [&](uint32_t c, f32x8 v, f32x8 w) {
     // 16 lanes hold a block; lanes behind the row's end hold zeros and take part in its maximum
-    const f32x8 w = load_weight8((const W *)a.weight, c, n, a.vec_w);
 #pragma unroll
     for (int i = 0; i < 8; i++) v[i] = v[i] * rstd * w[i];
     if (a.y && c < n) store8((T *)a.y + row * a.ld_y, c, n, a.vec, v);
@@ -105,19 +80,50 @@ __global__ __launch_bounds__(NT) void k_norm_quant(NormFwd a, uint64_t row0) {
       }
     }
   };
-  if (NV) {
+  if constexpr (NV > 0) {
+    V vx[NV], vr[NV];
+    typename Vec8<W>::type vw[NV];
+    f32x8 h[NV];
 #pragma unroll
-    for (int k = 0; k < NR; k++) {
+    for (int k = 0; k < NV; k++) {
       const uint32_t c = (k * NT + t) * 8;
-      if ((c & ~(kBlk - 1)) < n) give(c, h[k]);
+      vx[k] = load8_raw<true>(x, c, n, a.vec);
+      if (res) vr[k] = load8_raw<true>(res, c, n, a.vec);
+    }
+#pragma unroll
+    for (int k = 0; k < NV; k++)
+      if (a.weight) vw[k] = load8_raw((const W *)a.weight, (k * NT + t) * 8, n, a.vec_w);
+#pragma unroll
+    for (int k = 0; k < NV; k++) {
+      const uint32_t c = (k * NT + t) * 8;
+      h[k] = add(vx[k], vr[k]);
+      if (sum && c < n) store8(sum, c, n, a.vec, h[k]);
+      square(h[k]);
+    }
+    rstd = 1.0f / sqrtf(group_sum<NT>(acc, s_sum) * a.inv_cols + a.eps);
+#pragma unroll
+    for (int k = 0; k < NV; k++) {
+      const uint32_t c = (k * NT + t) * 8;
+      if ((c & ~(kBlk - 1)) < n) give(c, h[k], a.weight ? float8_of(vw[k]) : (f32x8){1, 1, 1, 1, 1, 1, 1, 1});
     }
   } else {
+    auto take = [&](uint32_t c) {
+      const V v = load8_raw(x, c, n, a.vec);
+      return add(v, res ? load8_raw(res, c, n, a.vec) : v);
+    };
+    for (uint32_t c = t * 8; c < n; c += NT * 8) {
+      const f32x8 h = take(c);
+      if (sum) store8(sum, c, n, a.vec, h);
+      square(h);
+    }
+    rstd = 1.0f / sqrtf(group_sum<NT>(acc, s_sum) * a.inv_cols + a.eps);
     for (uint32_t c = t * 8; (c & ~(kBlk - 1)) < n; c += NT * 8) {
-      f32x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
-      if (c < n) v = sum ? load8((const T *)sum, c, n, a.vec) : take(c);
-      give(c, v);
+      f32x8 h = {0, 0, 0, 0, 0, 0, 0, 0};
+      if (c < n) h = sum ? load8((const T *)sum, c, n, a.vec) : take(c);
+      give(c, h, weight8(c));
     }
   }
+  if (a.rstd && t == 0) a.rstd[row] = rstd;
 }
 
 struct NormBwd {
@@ -132,103 +138,133 @@ struct NormBwd {
   int vec, vec_w;
 };
 
-// Rows blockIdx.x, blockIdx.x + gridDim.x, ... ; the columns' sums stay in registers from row to row.  NV = 0: rows of any
-// length, read twice, their sums added up in the partial row in memory, which each thread alone touches at its columns.
+// Rows blockIdx.x, blockIdx.x + gridDim.x, ... ; the next row is requested before this one's sums, and the columns' sums stay
+// in registers from row to row.  NV = 0: rows of any length, read twice, their sums added up in the partial row in memory,
+// which each thread alone touches at its columns.
 template <typename T, typename W, int NT, int NV>
 __global__ __launch_bounds__(NT) void k_norm_bwd(NormBwd a) {
+  typedef typename Vec8<T>::type V;
   __shared__ float s_sum[2][NT / 64];
   const uint32_t t = threadIdx.x, n = a.cols;
-  constexpr int NR = NV ? NV : 1;
-  f32x8 dw[NR], w[NR];
-#pragma unroll
-  for (int k = 0; k < NR; k++) {
-    dw[k] = (f32x8){0, 0, 0, 0, 0, 0, 0, 0};
-    const uint32_t c = (k * NT + t) * 8;
-    if (NV && c < n) w[k] = load_weight8((const W *)a.weight, c, n, a.vec_w);
-  }
   float *part = a.part ? a.part + (uint64_t)blockIdx.x * n : nullptr;
-  int turn = 0;
-  for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
-    const T *pdy = (const T *)a.dy + row * a.ld_dy, *ph = (const T *)a.h + row * a.ld_h;
-    const T *pds = a.dsum ? (const T *)a.dsum + row * a.ld_dsum : nullptr;
-    T *pdx = (T *)a.dx + row * a.ld_dx;
-    const float rstd = a.rstd[row];
-    float acc = 0;
-    f32x8 xh[NR], g[NR];
-    auto step = [&](uint32_t c, f32x8 wv, f32x8 &xhv, f32x8 &gv, f32x8 &dwv) {
-      const f32x8 dy = load8(pdy, c, n, a.vec), h = load8(ph, c, n, a.vec);
+  float acc = 0, rstd = 0;
+  // one vector: xh, g, their product's share of the row's sum, and the weight gradient's share
+  auto step = [&](V vdy, V vh, f32x8 w, f32x8 &xh, f32x8 &g, f32x8 &dw) {
 #pragma unroll
-      for (int i = 0; i < 8; i++) {
-        xhv[i] = h[i] * rstd;
-        gv[i] = dy[i] * wv[i];
-        dwv[i] = __builtin_fmaf(dy[i], xhv[i], dwv[i]);
-        acc = __builtin_fmaf(gv[i], xhv[i], acc);
-      }
-    };
-    auto give = [&](uint32_t c, f32x8 xhv, f32x8 gv, float m) {
-      f32x8 d = {0, 0, 0, 0, 0, 0, 0, 0};
-      if (pds) d = load8(pds, c, n, a.vec);
+    for (int i = 0; i < 8; i++) {
+      const float dy = (float)vdy[i];
+      xh[i] = (float)vh[i] * rstd;
+      g[i] = dy * w[i];
+      dw[i] = __builtin_fmaf(dy, xh[i], dw[i]);
+      acc = __builtin_fmaf(g[i], xh[i], acc);
+    }
+  };
+  auto give = [&](uint64_t row, uint32_t c, f32x8 xh, f32x8 g, f32x8 d, float m) {
 #pragma unroll
-      for (int i = 0; i < 8; i++) d[i] = __builtin_fmaf(rstd, __builtin_fmaf(-xhv[i], m, gv[i]), d[i]);
-      store8(pdx, c, n, a.vec, d);
-    };
-    if (NV) {
+    for (int i = 0; i < 8; i++) d[i] = __builtin_fmaf(rstd, __builtin_fmaf(-xh[i], m, g[i]), d[i]);
+    store8((T *)a.dx + row * a.ld_dx, c, n, a.vec, d);
+  };
+  const f32x8 zero = {0, 0, 0, 0, 0, 0, 0, 0}, one = {1, 1, 1, 1, 1, 1, 1, 1};
+  int turn = 0;  // two sets of partial sums in turn: a wave writes the next row's while another still reads this one's
+  if constexpr (NV > 0) {
+    V vdy[NV], vh[NV], vds[NV];
+    typename Vec8<W>::type vw[NV];
+    f32x8 dw[NV];
+    auto request = [&](uint64_t row) {
 #pragma unroll
-      for (int k = 0; k < NR; k++) {
+      for (int k = 0; k < NV; k++) {
         const uint32_t c = (k * NT + t) * 8;
-        if (c < n) step(c, w[k], xh[k], g[k], dw[k]);
+        vdy[k] = load8_raw<true>((const T *)a.dy + row * a.ld_dy, c, n, a.vec);
+        vh[k] = load8_raw<true>((const T *)a.h + row * a.ld_h, c, n, a.vec);
+        if (a.dsum) vds[k] = load8_raw<true>((const T *)a.dsum + row * a.ld_dsum, c, n, a.vec);
       }
-    } else {
+    };
+#pragma unroll
+    for (int k = 0; k < NV; k++) {
+      dw[k] = zero;
+      if (a.weight) vw[k] = load8_raw((const W *)a.weight, (k * NT + t) * 8, n, a.vec_w);
+    }
+    request(blockIdx.x);
+    float next_rstd = a.rstd[blockIdx.x];
+    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+      f32x8 xh[NV], g[NV], d[NV];
+      acc = 0;
+      rstd = next_rstd;
+#pragma unroll
+      for (int k = 0; k < NV; k++) {
+        step(vdy[k], vh[k], a.weight ? float8_of(vw[k]) : one, xh[k], g[k], dw[k]);
+        d[k] = a.dsum ? float8_of(vds[k]) : zero;
+      }
+      if (row + gridDim.x < a.rows) {
+        request(row + gridDim.x);
+        next_rstd = a.rstd[row + gridDim.x];
+      }
+      const float m = group_sum<NT>(acc, s_sum[turn]) * a.inv_cols;
+#pragma unroll
+      for (int k = 0; k < NV; k++) {
+        const uint32_t c = (k * NT + t) * 8;
+        if (c < n) give(row, c, xh[k], g[k], d[k], m);
+      }
+    }
+    if (part) {
+#pragma unroll
+      for (int k = 0; k < NV; k++) {
+        const uint32_t c = (k * NT + t) * 8;
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+          if (c + i < n) part[c + i] = dw[k][i];
+      }
+    }
+  } else {
+    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+      const T *pdy = (const T *)a.dy + row * a.ld_dy, *ph = (const T *)a.h + row * a.ld_h;
+      f32x8 xh, g;
+      acc = 0;
+      rstd = a.rstd[row];
       for (uint32_t c = t * 8; c < n; c += NT * 8) {
-        f32x8 d = {0, 0, 0, 0, 0, 0, 0, 0}, xv, gv;
-        step(c, load_weight8((const W *)a.weight, c, n, a.vec_w), xv, gv, d);
+        f32x8 d = zero;
+        step(load8_raw(pdy, c, n, a.vec), load8_raw(ph, c, n, a.vec), a.weight ? load8((const W *)a.weight, c, n, a.vec_w) : one, xh, g, d);
         if (part) {
 #pragma unroll
           for (int i = 0; i < 8; i++)
             if (c + i < n) part[c + i] = (row == blockIdx.x ? 0.0f : part[c + i]) + d[i];
         }
       }
-    }
-    // two sets of partial sums in turn: a wave writes the next row's while another still reads this one's
-    const float m = group_sum<NT>(acc, s_sum[turn]) * a.inv_cols;
-    if (NV) {
-#pragma unroll
-      for (int k = 0; k < NR; k++) {
-        const uint32_t c = (k * NT + t) * 8;
-        if (c < n) give(c, xh[k], g[k], m);
-      }
-    } else {
+      const float m = group_sum<NT>(acc, s_sum[turn]) * a.inv_cols;
       for (uint32_t c = t * 8; c < n; c += NT * 8) {
-        f32x8 xv, gv, d;
-        const f32x8 wv = load_weight8((const W *)a.weight, c, n, a.vec_w), dy = load8(pdy, c, n, a.vec), h = load8(ph, c, n, a.vec);
-        (void)d;
-#pragma unroll
-        for (int i = 0; i < 8; i++) xv[i] = h[i] * rstd, gv[i] = dy[i] * wv[i];
-        give(c, xv, gv, m);
+        f32x8 unused = zero;
+        step(load8_raw(pdy, c, n, a.vec), load8_raw(ph, c, n, a.vec), a.weight ? load8((const W *)a.weight, c, n, a.vec_w) : one, xh, g, unused);
+        give(row, c, xh, g, a.dsum ? load8((const T *)a.dsum + row * a.ld_dsum, c, n, a.vec) : zero, m);
       }
-    }
-  }
-  if (NV && part) {
-#pragma unroll
-    for (int k = 0; k < NR; k++) {
-      const uint32_t c = (k * NT + t) * 8;
-#pragma unroll
-      for (int i = 0; i < 8; i++)
-        if (c + i < n) part[c + i] = dw[k][i];
     }
   }
 }
 
-// dw[c] = sum of the partial rows, in a fixed order: 64 columns a work-group, a quarter of the rows a wave.
-__global__ __launch_bounds__(kWG) void k_norm_dw(const float *__restrict__ part, uint32_t n_part, uint32_t cols, float *__restrict__ dw) {
-  __shared__ float s[kWG];
-  const uint32_t t = threadIdx.x, c = blockIdx.x * 64 + (t & 63);
+// dw[c] = sum of the partial rows, in a fixed order: 32 columns a work-group, every 32nd partial row a half wave, eight of
+// them requested at a time.
+constexpr int kDwWG = 1024;
+__global__ __launch_bounds__(kDwWG) void k_norm_dw(const float *__restrict__ part, uint32_t n_part, uint32_t cols, float *__restrict__ dw) {
+  __shared__ float s[kDwWG];
+  const uint32_t t = threadIdx.x, c = blockIdx.x * 32 + (t & 31), first = t >> 5;
+  constexpr uint32_t step = kDwWG / 32;
   float v = 0;
-  if (c < cols)
-    for (uint32_t p = t >> 6; p < n_part; p += kWG / 64) v += part[(uint64_t)p * cols + c];
+  if (c < cols) {
+    for (uint32_t p = first; p < n_part; p += 8 * step) {
+      float q[8];
+#pragma unroll
+      for (int k = 0; k < 8; k++) q[k] = p + k * step < n_part ? part[(uint64_t)(p + k * step) * cols + c] : 0.0f;
+#pragma unroll
+      for (int k = 0; k < 8; k++) v += q[k];
+    }
+  }
   s[t] = v;
   __syncthreads();
-  if (t < 64 && c < cols) dw[c] = (s[t] + s[t + 64]) + (s[t + 128] + s[t + 192]);
+  if (t < 32 && c < cols) {
+    float r = 0;
+#pragma unroll
+    for (uint32_t k = 0; k < step; k++) r += s[k * 32 + t];
+    dw[c] = r;
+  }
 }
 
 }  // namespace
