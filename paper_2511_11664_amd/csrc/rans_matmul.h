@@ -300,14 +300,21 @@ __device__ __forceinline__ void mm_step(const uint8_t *__restrict__ code, const 
       sb4[(i + 1) % 3] = scale4(i + 1);
     }
     __builtin_amdgcn_sched_barrier(0);
-    Bf16Operand wb;
-    if (EXACT) wb = widen<FB>(fb);
+    if (EXACT) {
+      const Bf16Operand wb = widen<FB>(fb);
 #pragma unroll
-    for (int j = 0; j < MT; j++) {
-      if (HW)
-        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb, fa[EXACT ? 0 : j], acc[i][j], FB, FA, 0, (int)sb8, 0, (int)sa[j]);
-      else
-        d[i & 1][j] = EXACT ? mfma_bf16(wb, wa[EXACT ? j : 0]) : mfma_8bit<FA, FB>(fb, fa[EXACT ? 0 : j]);
+      for (int q = 0; q < 4; q++)  // a sum's four steps depend on one another: in turn with the other sums'
+#pragma unroll
+        for (int j = 0; j < MT; j++)
+          d[i & 1][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb.q[q], wa[EXACT ? j : 0].q[q], q ? d[i & 1][j] : (f32x4){0, 0, 0, 0}, 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int j = 0; j < MT; j++) {
+        if (HW)
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb, fa[EXACT ? 0 : j], acc[i][j], FB, FA, 0, (int)sb8, 0, (int)sa[j]);
+        else
+          d[i & 1][j] = mfma_8bit<FA, FB>(fb, fa[EXACT ? 0 : j]);
+      }
     }
     if (!HW && i > 0) apply(i - 1);
     __builtin_amdgcn_sched_barrier(0);

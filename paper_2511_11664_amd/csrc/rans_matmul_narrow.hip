@@ -14,7 +14,9 @@
 #include "rans_matmul.h"
 #include "rans_matmul_pick.h"
 
-// Tiles by the least estimate.  B in E5M2, which no path of a training step has, takes the 128 x 128 tiles at every size.
+// Tiles by the least estimate.  B in E5M2, which no path of a training step has, takes the 128 x 128 tiles at every size.  The
+// large tiles are not for binary32 scales of both operands' rows, which leave them too few registers (4096 x 4096 x 11231: 574
+// us, 128 x 128 tiles 347).
 int launch_matmul_narrow(const MatmulArgs &p, int fmt, hipStream_t st) {
   const uint32_t units = compute_units() ? compute_units() : 256;
   const double large = mm_cost_large(p, units), medium = mm_cost_medium(p, units), small = mm_cost_small(p, units);
@@ -26,8 +28,9 @@ int launch_matmul_narrow(const MatmulArgs &p, int fmt, hipStream_t st) {
       if (few) return launch_few<2, 8, 4, FA, FB, SCALE, false>(p, st);
       if (!fetch) return launch_any<MmWide, FA, FB, SCALE, false>(p, st);
       if constexpr (FB == 0) {
-        if (small <= medium && small <= large) return launch_tiles<MmSmall, FA, FB, SCALE, false>(p, st);
-        if (large < medium) return launch_tiles<MmLarge, FA, FB, SCALE, false>(p, st);
+        if (small <= medium && (small <= large || SCALE == MM_F32_ROW)) return launch_tiles<MmSmall, FA, FB, SCALE, false>(p, st);
+        if constexpr (SCALE != MM_F32_ROW)
+          if (large < medium) return launch_tiles<MmLarge, FA, FB, SCALE, false>(p, st);
       }
       return launch_tiles<MmMedium, FA, FB, SCALE, false>(p, st);
     });
