@@ -28,23 +28,26 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // ------------------------------------------------------------------ element types: eight neighbours at a time
 
+// Aligned to an element only: the loads and stores stay 16 bytes wide, and cost more where they cross a cache line.
 template <typename T> struct Vec8;
-template <> struct Vec8<float> { typedef float type __attribute__((ext_vector_type(8), aligned(16))); };
-template <> struct Vec8<_Float16> { typedef _Float16 type __attribute__((ext_vector_type(8), aligned(16))); };
-template <> struct Vec8<__bf16> { typedef __bf16 type __attribute__((ext_vector_type(8), aligned(16))); };
+template <> struct Vec8<float> { typedef float type __attribute__((ext_vector_type(8), aligned(4))); };
+template <> struct Vec8<_Float16> { typedef _Float16 type __attribute__((ext_vector_type(8), aligned(2))); };
+template <> struct Vec8<__bf16> { typedef __bf16 type __attribute__((ext_vector_type(8), aligned(2))); };
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
 
-// Elements c .. c + 7 of a row of n as they lie in memory; those from n on are zero.  `vec`: rows start on 16 bytes.
+// Elements c .. c + 7 of a row of n as they lie in memory; those from n on are zero.
 // ONCE: read past the caches, for what nobody reads again soon (16384 x 4096 fp16 to codes: 41.6 -> 34.3 us, with two
 // blocks instead of four for a lane).
-template <bool ONCE = false, typename T> __device__ inline typename Vec8<T>::type load8_raw(const T *row, uint32_t c, uint32_t n, bool vec) {
+template <bool ONCE = false, typename T> __device__ inline typename Vec8<T>::type load8_raw(const T *row, uint32_t c, uint32_t n) {
   typedef typename Vec8<T>::type V;
-  if (vec && c + 8 <= n) {
+  if (c + 8 <= n) {
     if (!ONCE) return *(const V *)(row + c);
     struct Words {
       u32x4 w[sizeof(V) / 16];
     } q;
 #pragma unroll
-    for (size_t i = 0; i < sizeof(V) / 16; i++) q.w[i] = __builtin_nontemporal_load((const u32x4 *)(row + c) + i);
+    for (size_t i = 0; i < sizeof(V) / 16; i++) q.w[i] = __builtin_nontemporal_load((const u32x4_any *)(row + c) + i);
     return __builtin_bit_cast(V, q);
   }
   V v;
@@ -58,13 +61,13 @@ template <typename V> __device__ inline f32x8 float8_of(V v) {
   for (int i = 0; i < 8; i++) r[i] = (float)v[i];
   return r;
 }
-template <bool ONCE = false, typename T> __device__ inline f32x8 load8(const T *row, uint32_t c, uint32_t n, bool vec) {
-  return float8_of(load8_raw<ONCE>(row, c, n, vec));
+template <bool ONCE = false, typename T> __device__ inline f32x8 load8(const T *row, uint32_t c, uint32_t n) {
+  return float8_of(load8_raw<ONCE>(row, c, n));
 }
 
 // The element type's rounding (to nearest even) of eight binary32 values, kept if in the row.
-template <typename T> __device__ inline void store8(T *row, uint32_t c, uint32_t n, bool vec, f32x8 v) {
-  if (vec && c + 8 <= n) {
+template <typename T> __device__ inline void store8(T *row, uint32_t c, uint32_t n, f32x8 v) {
+  if (c + 8 <= n) {
     typename Vec8<T>::type o;
 #pragma unroll
     for (int i = 0; i < 8; i++) o[i] = (T)v[i];
@@ -168,19 +171,19 @@ __device__ inline f32x8 values8(u32x2 w, uint32_t e5m2) {
   return r;
 }
 
-__device__ inline void store_codes8(uint8_t *row, uint32_t c, uint32_t n, bool vec, u32x2 w) {
-  if (vec && c + 8 <= n) {
-    *(u32x2 *)(row + c) = w;
+__device__ inline void store_codes8(uint8_t *row, uint32_t c, uint32_t n, u32x2 w) {
+  if (c + 8 <= n) {
+    *(u32x2_any *)(row + c) = w;
   } else {
 #pragma unroll
     for (int i = 0; i < 8; i++)
       if (c + i < n) row[c + i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
   }
 }
-__device__ inline u32x2 load_codes8(const uint8_t *row, uint32_t c, uint32_t n, bool vec) {
+__device__ inline u32x2 load_codes8(const uint8_t *row, uint32_t c, uint32_t n) {
   u32x2 w = {0, 0};
-  if (vec && c + 8 <= n) {
-    w = *(const u32x2 *)(row + c);
+  if (c + 8 <= n) {
+    w = *(const u32x2_any *)(row + c);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; i++)
@@ -227,7 +230,7 @@ constexpr int kQuantUnits = 2;
 template <typename T, bool E8M0>
 __global__ __launch_bounds__(kWG) void k_block_quant(const T *__restrict__ x, uint64_t ld_x, uint8_t *__restrict__ codes, uint64_t ld,
                                                      void *__restrict__ scales, uint64_t ld_scale, uint32_t n_units, uint32_t cols,
-                                                     uint32_t nb, FastDivU32 by_nb, uint32_t e5m2, int vec_x, int vec_c) {
+                                                     uint32_t nb, FastDivU32 by_nb, uint32_t e5m2) {
   const uint32_t lane = threadIdx.x & 15, grp = threadIdx.x >> 4;
   const uint32_t u0 = blockIdx.x * (kWG / 16 * kQuantUnits) + grp;
   f32x8 v[kQuantUnits];
@@ -237,13 +240,13 @@ __global__ __launch_bounds__(kWG) void k_block_quant(const T *__restrict__ x, ui
     const uint32_t u = u0 + i * (kWG / 16);
     row[i] = by_nb(u < n_units ? u : 0);
     kb[i] = (u < n_units ? u : 0) - row[i] * nb;
-    v[i] = load8<true>(x + row[i] * ld_x, kb[i] * kBlk + lane * 8, cols, vec_x);
+    v[i] = load8<true>(x + row[i] * ld_x, kb[i] * kBlk + lane * 8, cols);
   }
 #pragma unroll
   for (int i = 0; i < kQuantUnits; i++) {
     if (u0 + i * (kWG / 16) >= n_units) break;
     const BlockScale s = block_scale<E8M0>(max16(abs_max8(v[i])), e5m2);
-    store_codes8(codes + row[i] * ld, kb[i] * kBlk + lane * 8, cols, vec_c, codes8(v[i], s.factor, e5m2));
+    store_codes8(codes + row[i] * ld, kb[i] * kBlk + lane * 8, cols, codes8(v[i], s.factor, e5m2));
     if (lane == 0) store_scale<E8M0>(scales, row[i] * ld_scale + kb[i], s);
   }
 }
@@ -255,7 +258,7 @@ __global__ __launch_bounds__(kWG) void k_block_quant(const T *__restrict__ x, ui
 template <typename T, bool E8M0, bool TRANS, bool TILE>
 __global__ __launch_bounds__(kWG) void k_block_quant_tile(const T *__restrict__ x, uint64_t ld_x, uint32_t x_rows, uint32_t x_cols,
                                                           uint8_t *__restrict__ codes, uint64_t ld, void *__restrict__ scales,
-                                                          uint64_t ld_scale, uint32_t e5m2, int vec_x, int vec_c) {
+                                                          uint64_t ld_scale, uint32_t e5m2) {
   __shared__ __attribute__((aligned(16))) uint8_t s_tile[TRANS ? kBlk * kBlk : 16];
   __shared__ uint32_t s_part[TILE ? kWG / 64 : 1];
   uint32_t *s_max = TILE ? s_part : (uint32_t *)s_tile;  // 16 groups' column maxima lie where the codes go later
@@ -267,7 +270,7 @@ __global__ __launch_bounds__(kWG) void k_block_quant_tile(const T *__restrict__ 
 #pragma unroll
   for (int i = 0; i < 8; i++) {
     const uint32_t r = r0 + grp * 8 + i;
-    v[i] = load8_raw<true>(x + (r < x_rows ? r : 0) * ld_x, c, r < x_rows ? x_cols : 0, vec_x);
+    v[i] = load8_raw<true>(x + (r < x_rows ? r : 0) * ld_x, c, r < x_rows ? x_cols : 0);
   }
   float factor[TILE ? 1 : 8];
   if (TILE) {
@@ -321,7 +324,7 @@ __global__ __launch_bounds__(kWG) void k_block_quant_tile(const T *__restrict__ 
 #pragma unroll
     for (int i = 0; i < 8; i++) {
       const uint32_t r = r0 + grp * 8 + i;
-      if (r < x_rows) store_codes8(codes + r * ld, c, x_cols, vec_c, codes8(float8_of(v[i]), factor[0], e5m2));
+      if (r < x_rows) store_codes8(codes + r * ld, c, x_cols, codes8(float8_of(v[i]), factor[0], e5m2));
     }
     return;
   }
@@ -343,11 +346,11 @@ __global__ __launch_bounds__(kWG) void k_block_quant_tile(const T *__restrict__ 
     if (turn & 1) w = (u32x4){w[2], w[3], w[0], w[1]};
     uint8_t *out = codes + (c0 + col) * ld;
     const uint32_t r = r0 + q * 16;
-    if (vec_c && r + 16 <= x_rows) {
-      *(u32x4 *)(out + r) = w;
+    if (r + 16 <= x_rows) {
+      __builtin_memcpy(out + r, &w, 16);
     } else {
-      store_codes8(out, r, x_rows, false, (u32x2){w[0], w[1]});
-      store_codes8(out, r + 8, x_rows, false, (u32x2){w[2], w[3]});
+      store_codes8(out, r, x_rows, (u32x2){w[0], w[1]});
+      store_codes8(out, r + 8, x_rows, (u32x2){w[2], w[3]});
     }
   }
 }
@@ -356,7 +359,7 @@ __global__ __launch_bounds__(kWG) void k_block_quant_tile(const T *__restrict__ 
 template <typename T, bool E8M0>
 __global__ __launch_bounds__(kWG) void k_block_dequant(const uint8_t *__restrict__ codes, uint64_t ld, const void *__restrict__ scales,
                                                        uint64_t ld_scale, T *__restrict__ x, uint64_t ld_x, uint32_t n_units, uint32_t cols,
-                                                       uint32_t nb, FastDivU32 by_nb, uint32_t tile, uint32_t e5m2, int vec_x, int vec_c) {
+                                                       uint32_t nb, FastDivU32 by_nb, uint32_t tile, uint32_t e5m2) {
   const uint32_t lane = threadIdx.x & 15, grp = threadIdx.x >> 4;
   const uint32_t u0 = blockIdx.x * (kWG / 16 * kQuantUnits) + grp;
   u32x2 w[kQuantUnits];
@@ -367,7 +370,7 @@ __global__ __launch_bounds__(kWG) void k_block_dequant(const uint8_t *__restrict
     const uint32_t u = u0 + i * (kWG / 16);
     row[i] = by_nb(u < n_units ? u : 0);
     kb[i] = (u < n_units ? u : 0) - row[i] * nb;
-    w[i] = load_codes8(codes + row[i] * ld, kb[i] * kBlk + lane * 8, cols, vec_c);
+    w[i] = load_codes8(codes + row[i] * ld, kb[i] * kBlk + lane * 8, cols);
     s[i] = load_scale<E8M0>(scales, (tile ? row[i] / kBlk : row[i]) * ld_scale + kb[i]);
   }
 #pragma unroll
@@ -376,7 +379,7 @@ __global__ __launch_bounds__(kWG) void k_block_dequant(const uint8_t *__restrict
     f32x8 v = values8(w[i], e5m2);
 #pragma unroll
     for (int j = 0; j < 8; j++) v[j] *= s[i];
-    store8(x + row[i] * ld_x, kb[i] * kBlk + lane * 8, cols, vec_x, v);
+    store8(x + row[i] * ld_x, kb[i] * kBlk + lane * 8, cols, v);
   }
 }
 

@@ -87,7 +87,6 @@ int rans_block_quantize(const void *d_x, uint64_t ld_x, uint32_t in_dtype, int t
   hipStream_t st = (hipStream_t)stream;
   const StreamDevice on(st);
   if (!on.ok) return RANS_ERR_HIP;
-  const int vec_x = aligned_to(d_x, 16) && ld_x * eb % 16 == 0;
   const bool tile = out->block == RANS_BLOCK_TILE;
   return by_dtype(in_dtype, [&](auto elem) {
     typedef decltype(elem) T;
@@ -95,7 +94,6 @@ int rans_block_quantize(const void *d_x, uint64_t ld_x, uint32_t in_dtype, int t
       constexpr bool E8M0 = decltype(e8m0_tag)::value;
       const T *x = (const T *)d_x;
       if (!transpose && !tile) {
-        const int vec_c = aligned_to(d_code, 8) && out->ld % 8 == 0;
         const uint64_t nb = (x_cols + kBlk - 1) / kBlk;
         const FastDivU32 by_nb = FastDivU32::of((uint32_t)nb);
         const uint64_t step = kQuantSliceUnits / nb;
@@ -104,12 +102,11 @@ int rans_block_quantize(const void *d_x, uint64_t ld_x, uint32_t in_dtype, int t
           const uint32_t g = (uint32_t)((units + kWG / 16 * kQuantUnits - 1) / (kWG / 16 * kQuantUnits));
           PROF_LAUNCH(KID_BLOCK_QUANT, (k_block_quant<T, E8M0>), dim3(g), dim3(kWG), 0, st, x + r * ld_x, ld_x, d_code + r * out->ld, out->ld,
                       (void *)((uint8_t *)d_scale + r * out->ld_scale * (E8M0 ? 1 : 4)), out->ld_scale, (uint32_t)units, (uint32_t)x_cols,
-                      (uint32_t)nb, by_nb, out->format, vec_x, vec_c);
+                      (uint32_t)nb, by_nb, out->format);
           LAUNCH_CHECK();
         }
         return RANS_OK;
       }
-      const int vec_c = transpose ? aligned_to(d_code, 16) && out->ld % 16 == 0 : aligned_to(d_code, 8) && out->ld % 8 == 0;
       for (uint64_t r = 0; r < x_rows; r += kQuantSliceRows) {
         const uint64_t rows = x_rows - r < kQuantSliceRows ? x_rows - r : kQuantSliceRows;
         const dim3 grid((uint32_t)((x_cols + kBlk - 1) / kBlk), (uint32_t)((rows + kBlk - 1) / kBlk));
@@ -118,7 +115,7 @@ int rans_block_quantize(const void *d_x, uint64_t ld_x, uint32_t in_dtype, int t
         uint8_t *scales = (uint8_t *)d_scale + (transpose ? r / kBlk : r / kBlk * out->ld_scale) * (E8M0 ? 1 : 4);
 #define TILE_LAUNCH(TRANS, TILE)                                                                                                   \
   PROF_LAUNCH(KID_BLOCK_QUANT_TILE, (k_block_quant_tile<T, E8M0, TRANS, TILE>), grid, dim3(kWG), 0, st, x + r * ld_x, ld_x, (uint32_t)rows, \
-              (uint32_t)x_cols, codes, out->ld, (void *)scales, out->ld_scale, out->format, vec_x, vec_c)
+              (uint32_t)x_cols, codes, out->ld, (void *)scales, out->ld_scale, out->format)
         if (!transpose) TILE_LAUNCH(false, true);
         else if (tile) TILE_LAUNCH(true, true);
         else TILE_LAUNCH(true, false);
@@ -142,7 +139,6 @@ int rans_block_dequantize(const uint8_t *d_code, const void *d_scale, const rans
   hipStream_t st = (hipStream_t)stream;
   const StreamDevice on(st);
   if (!on.ok) return RANS_ERR_HIP;
-  const int vec_x = aligned_to(d_x_out, 16) && ld_x * eb % 16 == 0, vec_c = aligned_to(d_code, 8) && in->ld % 8 == 0;
   const uint32_t tile = in->block == RANS_BLOCK_TILE;
   return by_dtype(out_dtype, [&](auto elem) {
     typedef decltype(elem) T;
@@ -157,7 +153,7 @@ int rans_block_dequantize(const uint8_t *d_code, const void *d_scale, const rans
         const uint64_t srow = tile ? r / kBlk : r;
         PROF_LAUNCH(KID_BLOCK_DEQUANT, (k_block_dequant<T, E8M0>), dim3(g), dim3(kWG), 0, st, d_code + r * in->ld, in->ld,
                     (const void *)((const uint8_t *)d_scale + srow * in->ld_scale * (E8M0 ? 1 : 4)), in->ld_scale, (T *)d_x_out + r * ld_x, ld_x,
-                    (uint32_t)units, (uint32_t)in->cols, (uint32_t)nb, by_nb, tile, in->format, vec_x, vec_c);
+                    (uint32_t)units, (uint32_t)in->cols, (uint32_t)nb, by_nb, tile, in->format);
         LAUNCH_CHECK();
       }
       return RANS_OK;
@@ -241,12 +237,8 @@ int rans_norm_quantize(const void *d_x, const void *d_res, const void *d_weight,
   a.x = d_x, a.res = d_res, a.weight = d_weight, a.sum = d_sum, a.y = d_y, a.rstd = d_rstd, a.codes = d_code, a.scales = d_scale;
   a.ld_x = p->ld_x, a.ld_res = p->ld_res, a.ld_sum = p->ld_sum, a.ld_y = p->ld_y;
   a.cols = (uint32_t)p->cols, a.eps = p->eps, a.inv_cols = 1.0f / (float)p->cols;
-  auto fits = [&](const void *q, uint64_t ld) { return !q || (aligned_to(q, 16) && ld * eb % 16 == 0); };
-  a.vec = fits(d_x, p->ld_x) && fits(d_res, p->ld_res) && fits(d_sum, p->ld_sum) && fits(d_y, p->ld_y);
-  a.vec_w = aligned_to(d_weight, 16);
   if (d_code) {
     a.ld = out->ld, a.ld_scale = out->ld_scale, a.e5m2 = out->format;
-    a.vec_c = aligned_to(d_code, 8) && out->ld % 8 == 0;
   }
   return by_dtype(p->dtype, [&](auto elem) {
     typedef decltype(elem) T;
@@ -302,9 +294,6 @@ int rans_norm_backward(const void *d_dy, const void *d_dsum, const void *d_sum, 
   a.part = d_dweight ? (float *)d_ws : nullptr;
   a.ld_dy = p->ld_y, a.ld_dsum = p->ld_res, a.ld_h = p->ld_sum, a.ld_dx = p->ld_x;
   a.rows = p->rows, a.cols = (uint32_t)p->cols, a.inv_cols = 1.0f / (float)p->cols;
-  auto fits = [&](const void *q, uint64_t ld) { return !q || (aligned_to(q, 16) && ld * eb % 16 == 0); };
-  a.vec = fits(d_dy, p->ld_y) && fits(d_dsum, p->ld_res) && fits(d_sum, p->ld_sum) && fits(d_dx, p->ld_x);
-  a.vec_w = aligned_to(d_weight, 16);
   const uint32_t g = norm_parts(*p);
   if (g) {
     rc = by_dtype(p->dtype, [&](auto elem) {
@@ -374,8 +363,7 @@ int rans_block_matmul(const uint8_t *d_a, const void *d_a_scale, const rans_bloc
   const StreamDevice on(st);
   if (!on.ok) return RANS_ERR_HIP;
   MatmulArgs p{d_a, d_b, d_a_scale, d_b_scale, d_c, a->ld, b->ld, a->ld_scale, b->ld_scale, ld_c, (uint32_t)a->rows, (uint32_t)b->rows,
-               (uint32_t)a->cols, a->scale_type == RANS_SCALE_E8M0, b->block == RANS_BLOCK_TILE, out_dtype,
-               aligned_to(d_c, 16) && ld_c * eb % 16 == 0 ? 2 : aligned_to(d_c, 4 * eb) && ld_c % 4 == 0};
+               (uint32_t)a->cols, a->scale_type == RANS_SCALE_E8M0, b->block == RANS_BLOCK_TILE, out_dtype};
   const int fmt = (a->format == RANS_E5M2 ? 2 : 0) + (b->format == RANS_E5M2 ? 1 : 0);
   return out_dtype == RANS_F32 ? launch_matmul_wide(p, fmt, st) : launch_matmul_narrow(p, fmt, st);
 }

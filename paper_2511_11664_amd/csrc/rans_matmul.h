@@ -69,18 +69,20 @@ __device__ inline float matmul_scale(const void *s, uint64_t at, uint32_t e8m0) 
 
 // ------------------------------------------------------------------ results
 
+template <int OUT> __device__ inline uint32_t pack2(float a, float b) {
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+  if (OUT == RANS_F16) return __builtin_bit_cast(uint32_t, (f16x2){(_Float16)a, (_Float16)b});
+  return __builtin_bit_cast(uint32_t, (bf16x2){(__bf16)a, (__bf16)b});
+}
 // Columns n .. n + 3 of row m.
 __device__ inline void store_c4(const MatmulArgs &p, uint32_t m, uint32_t n, f32x4 v) {
   const uint64_t at = m * p.ldc + n;
-  if (p.vec_c && n + 4 <= p.n) {
+  if (n + 4 <= p.n) {  // at once, wherever the row starts
     if (p.out == RANS_F32) {
-      *(f32x4 *)((float *)p.c + at) = v;
-    } else if (p.out == RANS_F16) {
-      typedef _Float16 h4 __attribute__((ext_vector_type(4)));
-      *(h4 *)((_Float16 *)p.c + at) = (h4){(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]};
+      __builtin_memcpy((float *)p.c + at, &v, 16);
     } else {
-      typedef __bf16 b4 __attribute__((ext_vector_type(4)));
-      *(b4 *)((__bf16 *)p.c + at) = (b4){(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+      const u32x2 w = p.out == RANS_F16 ? (u32x2){pack2<RANS_F16>(v[0], v[1]), pack2<RANS_F16>(v[2], v[3])} : (u32x2){pack2<RANS_BF16>(v[0], v[1]), pack2<RANS_BF16>(v[2], v[3])};
+      __builtin_memcpy((uint16_t *)p.c + at, &w, 8);
     }
     return;
   }
@@ -93,11 +95,6 @@ __device__ inline void store_c4(const MatmulArgs &p, uint32_t m, uint32_t n, f32
   }
 }
 
-template <int OUT> __device__ inline uint32_t pack2(float a, float b) {
-  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-  if (OUT == RANS_F16) return __builtin_bit_cast(uint32_t, (f16x2){(_Float16)a, (_Float16)b});
-  return __builtin_bit_cast(uint32_t, (bf16x2){(__bf16)a, (__bf16)b});
-}
 // A wave's part of a tile that lies inside C, 16-bit results: two neighbouring operands' results change places between
 // lanes, so that a lane holds eight neighbouring columns and a row gets 64 bytes at once (32 without: 4096 x 8192 x 4096
 // with power-of-two scales 146 -> 114 us).
@@ -109,7 +106,8 @@ template <int OUT, int NT, int MT> __device__ inline void store_c16(const Matmul
     for (int i = 0; i < NT; i += 2) {
       const auto lo = __builtin_amdgcn_permlane16_swap(pack2<OUT>(acc[i][j][0], acc[i][j][1]), pack2<OUT>(acc[i + 1][j][0], acc[i + 1][j][1]), false, false);
       const auto hi = __builtin_amdgcn_permlane16_swap(pack2<OUT>(acc[i][j][2], acc[i][j][3]), pack2<OUT>(acc[i + 1][j][2], acc[i + 1][j][3]), false, false);
-      *(u32x4 *)(row + i * 16) = (u32x4){lo[0], hi[0], lo[1], hi[1]};
+      const u32x4 w = {lo[0], hi[0], lo[1], hi[1]};
+      __builtin_memcpy(row + i * 16, &w, 16);
     }
   }
 }
@@ -333,7 +331,7 @@ __device__ __forceinline__ void mm_step(const uint8_t *__restrict__ code, const 
 template <typename TILE> __device__ __forceinline__ void mm_store(const MatmulArgs &p, uint32_t m0, uint32_t n0, uint32_t wm, uint32_t wn, uint32_t lane, const f32x4 (&acc)[TILE::nt][TILE::mt]) {
   constexpr int NT = TILE::nt, MT = TILE::mt;
   const uint32_t g = lane >> 4, m = m0 + wm * MT * 16 + (lane & 15), n = n0 + wn * NT * 16;
-  if (p.vec_c == 2 && p.out != RANS_F32 && m0 + TILE::bm <= p.m && n0 + TILE::bn <= p.n) {
+  if (p.out != RANS_F32 && m0 + TILE::bm <= p.m && n0 + TILE::bn <= p.n) {
     if (p.out == RANS_F16) store_c16<RANS_F16>(p, m, n, g, acc);
     else store_c16<RANS_BF16>(p, m, n, g, acc);
     return;

@@ -13,7 +13,6 @@ struct MatmulArgs {
   uint32_t m, n, k;
   uint32_t e8m0, b_tile;
   uint32_t out;  // RANS_F32 / F16 / BF16
-  int vec_c;     // C's rows start on four elements (1), on 16 bytes (2)
 };
 
 // fmt: 2 where A's codes are E5M2, and 1 where B's are.  Results of 16 bits / binary32 results.

@@ -39,7 +39,6 @@ struct NormFwd {
   uint64_t ld_x, ld_res, ld_sum, ld_y, ld, ld_scale;
   uint32_t cols, e5m2;
   float eps, inv_cols;
-  int vec, vec_w, vec_c;  // every row of the streams / the weight / the codes may be taken 16 (codes: 8) bytes at a time
 };
 
 // A row per work-group of NT threads, NV times eight neighbouring elements a thread (NV = 0: any length, h read again).
@@ -66,16 +65,16 @@ __global__ __launch_bounds__(NT) void k_norm_quant(NormFwd a, uint64_t row0) {
 #pragma unroll
     for (int i = 0; i < 8; i++) acc = __builtin_fmaf(h[i], h[i], acc);
   };
-  auto weight8 = [&](uint32_t c) { return a.weight ? load8((const W *)a.weight, c, n, a.vec_w) : (f32x8){1, 1, 1, 1, 1, 1, 1, 1}; };
+  auto weight8 = [&](uint32_t c) { return a.weight ? load8((const W *)a.weight, c, n) : (f32x8){1, 1, 1, 1, 1, 1, 1, 1}; };
   auto give = [&](uint32_t c, f32x8 v, f32x8 w) {
     // 16 lanes hold a block; lanes behind the row's end hold zeros and take part in its maximum
 #pragma unroll
     for (int i = 0; i < 8; i++) v[i] = v[i] * rstd * w[i];
-    if (a.y && c < n) store8((T *)a.y + row * a.ld_y, c, n, a.vec, v);
+    if (a.y && c < n) store8((T *)a.y + row * a.ld_y, c, n, v);
     if (a.codes) {
       const BlockScale s = block_scale<E8M0>(max16(abs_max8(v)), a.e5m2);
       if (c < n) {
-        store_codes8(a.codes + row * a.ld, c, n, a.vec_c, codes8(v, s.factor, a.e5m2));
+        store_codes8(a.codes + row * a.ld, c, n, codes8(v, s.factor, a.e5m2));
         if ((t & 15) == 0) store_scale<E8M0>(a.scales, row * a.ld_scale + c / kBlk, s);
       }
     }
@@ -87,17 +86,17 @@ __global__ __launch_bounds__(NT) void k_norm_quant(NormFwd a, uint64_t row0) {
 #pragma unroll
     for (int k = 0; k < NV; k++) {
       const uint32_t c = (k * NT + t) * 8;
-      vx[k] = load8_raw<true>(x, c, n, a.vec);
-      if (res) vr[k] = load8_raw<true>(res, c, n, a.vec);
+      vx[k] = load8_raw<true>(x, c, n);
+      if (res) vr[k] = load8_raw<true>(res, c, n);
     }
 #pragma unroll
     for (int k = 0; k < NV; k++)
-      if (a.weight) vw[k] = load8_raw((const W *)a.weight, (k * NT + t) * 8, n, a.vec_w);
+      if (a.weight) vw[k] = load8_raw((const W *)a.weight, (k * NT + t) * 8, n);
 #pragma unroll
     for (int k = 0; k < NV; k++) {
       const uint32_t c = (k * NT + t) * 8;
       h[k] = add(vx[k], vr[k]);
-      if (sum && c < n) store8(sum, c, n, a.vec, h[k]);
+      if (sum && c < n) store8(sum, c, n, h[k]);
       square(h[k]);
     }
     rstd = 1.0f / sqrtf(group_sum<NT>(acc, s_sum) * a.inv_cols + a.eps);
@@ -108,18 +107,18 @@ __global__ __launch_bounds__(NT) void k_norm_quant(NormFwd a, uint64_t row0) {
     }
   } else {
     auto take = [&](uint32_t c) {
-      const V v = load8_raw(x, c, n, a.vec);
-      return add(v, res ? load8_raw(res, c, n, a.vec) : v);
+      const V v = load8_raw(x, c, n);
+      return add(v, res ? load8_raw(res, c, n) : v);
     };
     for (uint32_t c = t * 8; c < n; c += NT * 8) {
       const f32x8 h = take(c);
-      if (sum) store8(sum, c, n, a.vec, h);
+      if (sum) store8(sum, c, n, h);
       square(h);
     }
     rstd = 1.0f / sqrtf(group_sum<NT>(acc, s_sum) * a.inv_cols + a.eps);
     for (uint32_t c = t * 8; (c & ~(kBlk - 1)) < n; c += NT * 8) {
       f32x8 h = {0, 0, 0, 0, 0, 0, 0, 0};
-      if (c < n) h = sum ? load8((const T *)sum, c, n, a.vec) : take(c);
+      if (c < n) h = sum ? load8((const T *)sum, c, n) : take(c);
       give(c, h, weight8(c));
     }
   }
@@ -135,7 +134,6 @@ struct NormBwd {
   uint64_t rows;
   uint32_t cols;
   float inv_cols;
-  int vec, vec_w;
 };
 
 // Rows blockIdx.x, blockIdx.x + gridDim.x, ... ; the next row is requested before this one's sums, and the columns' sums stay
@@ -162,7 +160,7 @@ __global__ __launch_bounds__(NT) void k_norm_bwd(NormBwd a) {
   auto give = [&](uint64_t row, uint32_t c, f32x8 xh, f32x8 g, f32x8 d, float m) {
 #pragma unroll
     for (int i = 0; i < 8; i++) d[i] = __builtin_fmaf(rstd, __builtin_fmaf(-xh[i], m, g[i]), d[i]);
-    store8((T *)a.dx + row * a.ld_dx, c, n, a.vec, d);
+    store8((T *)a.dx + row * a.ld_dx, c, n, d);
   };
   const f32x8 zero = {0, 0, 0, 0, 0, 0, 0, 0}, one = {1, 1, 1, 1, 1, 1, 1, 1};
   int turn = 0;  // two sets of partial sums in turn: a wave writes the next row's while another still reads this one's
@@ -174,15 +172,15 @@ __global__ __launch_bounds__(NT) void k_norm_bwd(NormBwd a) {
 #pragma unroll
       for (int k = 0; k < NV; k++) {
         const uint32_t c = (k * NT + t) * 8;
-        vdy[k] = load8_raw<true>((const T *)a.dy + row * a.ld_dy, c, n, a.vec);
-        vh[k] = load8_raw<true>((const T *)a.h + row * a.ld_h, c, n, a.vec);
-        if (a.dsum) vds[k] = load8_raw<true>((const T *)a.dsum + row * a.ld_dsum, c, n, a.vec);
+        vdy[k] = load8_raw<true>((const T *)a.dy + row * a.ld_dy, c, n);
+        vh[k] = load8_raw<true>((const T *)a.h + row * a.ld_h, c, n);
+        if (a.dsum) vds[k] = load8_raw<true>((const T *)a.dsum + row * a.ld_dsum, c, n);
       }
     };
 #pragma unroll
     for (int k = 0; k < NV; k++) {
       dw[k] = zero;
-      if (a.weight) vw[k] = load8_raw((const W *)a.weight, (k * NT + t) * 8, n, a.vec_w);
+      if (a.weight) vw[k] = load8_raw((const W *)a.weight, (k * NT + t) * 8, n);
     }
     request(blockIdx.x);
     float next_rstd = a.rstd[blockIdx.x];
@@ -223,7 +221,7 @@ __global__ __launch_bounds__(NT) void k_norm_bwd(NormBwd a) {
       rstd = a.rstd[row];
       for (uint32_t c = t * 8; c < n; c += NT * 8) {
         f32x8 d = zero;
-        step(load8_raw(pdy, c, n, a.vec), load8_raw(ph, c, n, a.vec), a.weight ? load8((const W *)a.weight, c, n, a.vec_w) : one, xh, g, d);
+        step(load8_raw(pdy, c, n), load8_raw(ph, c, n), a.weight ? load8((const W *)a.weight, c, n) : one, xh, g, d);
         if (part) {
 #pragma unroll
           for (int i = 0; i < 8; i++)
@@ -233,8 +231,8 @@ __global__ __launch_bounds__(NT) void k_norm_bwd(NormBwd a) {
       const float m = group_sum<NT>(acc, s_sum[turn]) * a.inv_cols;
       for (uint32_t c = t * 8; c < n; c += NT * 8) {
         f32x8 unused = zero;
-        step(load8_raw(pdy, c, n, a.vec), load8_raw(ph, c, n, a.vec), a.weight ? load8((const W *)a.weight, c, n, a.vec_w) : one, xh, g, unused);
-        give(row, c, xh, g, a.dsum ? load8((const T *)a.dsum + row * a.ld_dsum, c, n, a.vec) : zero, m);
+        step(load8_raw(pdy, c, n), load8_raw(ph, c, n), a.weight ? load8((const W *)a.weight, c, n) : one, xh, g, unused);
+        give(row, c, xh, g, a.dsum ? load8((const T *)a.dsum + row * a.ld_dsum, c, n) : zero, m);
       }
     }
   }
