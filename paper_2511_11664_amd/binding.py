@@ -316,12 +316,17 @@ def _at(t):
     return None if t is None else t.data_ptr()
 
 
-def _holds(t, rows, cols, ld):
-    """Whether a tensor's memory reaches to the end of rows x cols elements that are ld apart; an absent one does."""
-    if t is None or not rows or not cols:
+def _holds(t, rows, cols, ld, size):
+    """Whether a tensor has elements of `size` bytes and its memory reaches to the end of rows x cols of them that are ld
+    apart; an absent one does."""
+    if t is None:
+        return True
+    if t.element_size() != size:
+        return False
+    if not rows or not cols:
         return True
     need = (rows - 1) * ld + cols
-    return need <= t.numel() or need <= _reach(t)
+    return need <= (t.numel() if t.is_contiguous() else _reach(t))
 
 
 def _reach(t):
@@ -336,28 +341,35 @@ def _reach(t):
 
 def _holds_blocks(code, scale, b):
     rows, cols = b.rows, b.cols
-    return _holds(code, rows, cols, b.ld) and _holds(scale, -(-rows // BLOCK) if b.block else rows, -(-cols // BLOCK), b.ld_scale)
+    return _holds(code, rows, cols, b.ld, 1) and _holds(scale, -(-rows // BLOCK) if b.block else rows, -(-cols // BLOCK), b.ld_scale,
+                                                        1 if b.scale_type else 4)
+
+
+def _size(dtype):
+    return 2 if dtype else 4
 
 
 def rans_block_quantize(d_x, ld_x, in_dtype, transpose, d_code, d_scale, out) -> int:
     st = _on(d_x, d_code, d_scale)
-    if st is None or not _holds_blocks(d_code, d_scale, out) or not _holds(d_x, *((out.cols, out.rows) if transpose else (out.rows, out.cols)), ld_x):
+    if st is None or not _holds_blocks(d_code, d_scale, out) or not _holds(d_x, *((out.cols, out.rows) if transpose else (out.rows, out.cols)), ld_x,
+                                                                                 _size(in_dtype)):
         return ERR_ARG
     return lib().rans_block_quantize(_at(d_x), ld_x, in_dtype, transpose, _at(d_code), _at(d_scale), out, st)
 
 
 def rans_block_dequantize(d_code, d_scale, blocks, out_dtype, d_x_out, ld_x) -> int:
     st = _on(d_x_out, d_code, d_scale)
-    if st is None or not _holds_blocks(d_code, d_scale, blocks) or not _holds(d_x_out, blocks.rows, blocks.cols, ld_x):
+    if st is None or not _holds_blocks(d_code, d_scale, blocks) or not _holds(d_x_out, blocks.rows, blocks.cols, ld_x, _size(out_dtype)):
         return ERR_ARG
     return lib().rans_block_dequantize(_at(d_code), _at(d_scale), blocks, out_dtype, _at(d_x_out), ld_x, st)
 
 
 def rans_norm_quantize(d_x, d_res, d_weight, p, d_sum, d_rstd, d_y, d_code, d_scale, out) -> int:
     st = _on(d_x, d_res, d_weight, d_sum, d_rstd, d_y, d_code, d_scale)
-    rows, cols = p.rows, p.cols
-    if st is None or not (_holds(d_x, rows, cols, p.ld_x) and _holds(d_res, rows, cols, p.ld_res) and _holds(d_sum, rows, cols, p.ld_sum)
-                          and _holds(d_y, rows, cols, p.ld_y) and _holds(d_weight, 1, cols, cols) and _holds(d_rstd, 1, rows, rows)
+    rows, cols, e = p.rows, p.cols, _size(p.dtype)
+    if st is None or not (_holds(d_x, rows, cols, p.ld_x, e) and _holds(d_res, rows, cols, p.ld_res, e) and _holds(d_sum, rows, cols, p.ld_sum, e)
+                          and _holds(d_y, rows, cols, p.ld_y, e) and _holds(d_weight, 1, cols, cols, _size(p.weight_dtype))
+                          and _holds(d_rstd, 1, rows, rows, 4)
                           and (d_code is None or (out is not None and _holds_blocks(d_code, d_scale, out)))):
         return ERR_ARG
     return lib().rans_norm_quantize(_at(d_x), _at(d_res), _at(d_weight), p, _at(d_sum), _at(d_rstd), _at(d_y), _at(d_code), _at(d_scale), out, st)
@@ -371,10 +383,10 @@ def rans_norm_workspace_bytes(p: NormParams):
 
 def rans_norm_backward(d_dy, d_dsum, d_sum, d_weight, d_rstd, p, d_dx, d_dweight, d_ws) -> int:
     st = _on(d_dy, d_dsum, d_sum, d_weight, d_rstd, d_dx, d_dweight, d_ws)
-    rows, cols = p.rows, p.cols
-    if st is None or not (_holds(d_dy, rows, cols, p.ld_y) and _holds(d_dsum, rows, cols, p.ld_res) and _holds(d_sum, rows, cols, p.ld_sum)
-                          and _holds(d_dx, rows, cols, p.ld_x) and _holds(d_weight, 1, cols, cols) and _holds(d_rstd, 1, rows, rows)
-                          and _holds(d_dweight, 1, cols, cols)):
+    rows, cols, e = p.rows, p.cols, _size(p.dtype)
+    if st is None or not (_holds(d_dy, rows, cols, p.ld_y, e) and _holds(d_dsum, rows, cols, p.ld_res, e) and _holds(d_sum, rows, cols, p.ld_sum, e)
+                          and _holds(d_dx, rows, cols, p.ld_x, e) and _holds(d_weight, 1, cols, cols, _size(p.weight_dtype))
+                          and _holds(d_rstd, 1, rows, rows, 4) and _holds(d_dweight, 1, cols, cols, 4)):
         return ERR_ARG
     return lib().rans_norm_backward(_at(d_dy), _at(d_dsum), _at(d_sum), _at(d_weight), _at(d_rstd), p, _at(d_dx), _at(d_dweight), _at(d_ws),
                                     0 if d_ws is None else d_ws.numel() * d_ws.element_size(), st)
@@ -388,7 +400,7 @@ def rans_matmul_workspace_bytes(a: Blocks, b: Blocks):
 
 def rans_block_matmul(d_a, d_a_scale, a, d_b, d_b_scale, b, out_dtype, d_c, ld_c, d_ws) -> int:
     st = _on(d_c, d_a, d_a_scale, d_b, d_b_scale, d_ws)
-    if st is None or not (_holds_blocks(d_a, d_a_scale, a) and _holds_blocks(d_b, d_b_scale, b) and _holds(d_c, a.rows, b.rows, ld_c)):
+    if st is None or not (_holds_blocks(d_a, d_a_scale, a) and _holds_blocks(d_b, d_b_scale, b) and _holds(d_c, a.rows, b.rows, ld_c, _size(out_dtype))):
         return ERR_ARG
     return lib().rans_block_matmul(_at(d_a), _at(d_a_scale), a, _at(d_b), _at(d_b_scale), b, out_dtype, _at(d_c), ld_c, _at(d_ws),
                                    0 if d_ws is None else d_ws.numel() * d_ws.element_size(), st)

@@ -355,11 +355,11 @@ __global__ __launch_bounds__(kWG) void k_block_quant_tile(const T *__restrict__ 
   }
 }
 
-// Codes times scales, rounded once to the output's type.
+// Codes times scales, rounded once to the output's type.  in_tile: where in its tile the first row lies.
 template <typename T, bool E8M0>
 __global__ __launch_bounds__(kWG) void k_block_dequant(const uint8_t *__restrict__ codes, uint64_t ld, const void *__restrict__ scales,
                                                        uint64_t ld_scale, T *__restrict__ x, uint64_t ld_x, uint32_t n_units, uint32_t cols,
-                                                       uint32_t nb, FastDivU32 by_nb, uint32_t tile, uint32_t e5m2) {
+                                                       uint32_t nb, FastDivU32 by_nb, uint32_t tile, uint32_t in_tile, uint32_t e5m2) {
   const uint32_t lane = threadIdx.x & 15, grp = threadIdx.x >> 4;
   const uint32_t u0 = blockIdx.x * (kWG / 16 * kQuantUnits) + grp;
   u32x2 w[kQuantUnits];
@@ -371,7 +371,7 @@ __global__ __launch_bounds__(kWG) void k_block_dequant(const uint8_t *__restrict
     row[i] = by_nb(u < n_units ? u : 0);
     kb[i] = (u < n_units ? u : 0) - row[i] * nb;
     w[i] = load_codes8(codes + row[i] * ld, kb[i] * kBlk + lane * 8, cols);
-    s[i] = load_scale<E8M0>(scales, (tile ? row[i] / kBlk : row[i]) * ld_scale + kb[i]);
+    s[i] = load_scale<E8M0>(scales, (tile ? (in_tile + row[i]) / kBlk : row[i]) * ld_scale + kb[i]);
   }
 #pragma unroll
   for (int i = 0; i < kQuantUnits; i++) {

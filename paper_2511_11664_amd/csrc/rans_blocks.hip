@@ -46,7 +46,7 @@ inline size_t elem_bytes(uint32_t dtype) { return dtype == RANS_F32 ? 4 : 2; }
 
 int check_blocks(const rans_blocks *b) {
   if (!b) return RANS_ERR_ARG;
-  if (b->format > RANS_E5M2 || b->scale_type > RANS_SCALE_E8M0 || b->block > RANS_BLOCK_TILE) return RANS_ERR_ARG;
+  if (b->format > RANS_E5M2 || b->scale_type > RANS_SCALE_E8M0 || b->block > RANS_BLOCK_TILE || b->reserved) return RANS_ERR_ARG;
   if (b->rows > kBlkMaxDim || b->cols > kBlkMaxDim || b->ld > kBlkMaxLd || b->ld_scale > kBlkMaxLd) return RANS_ERR_ARG;
   if (b->ld < b->cols || b->ld_scale < (b->cols + kBlk - 1) / kBlk) return RANS_ERR_SHAPE;
   return RANS_OK;
@@ -146,14 +146,14 @@ int rans_block_dequantize(const uint8_t *d_code, const void *d_scale, const rans
       constexpr bool E8M0 = decltype(e8m0_tag)::value;
       const uint64_t nb = (in->cols + kBlk - 1) / kBlk;
       const FastDivU32 by_nb = FastDivU32::of((uint32_t)nb);
-      const uint64_t step = kQuantSliceUnits / nb / kBlk * kBlk;  // slices start on a tile
+      const uint64_t step = kQuantSliceUnits / nb;
       for (uint64_t r = 0; r < in->rows; r += step) {
         const uint64_t rows = in->rows - r < step ? in->rows - r : step, units = rows * nb;
         const uint32_t g = (uint32_t)((units + kWG / 16 * kQuantUnits - 1) / (kWG / 16 * kQuantUnits));
         const uint64_t srow = tile ? r / kBlk : r;
         PROF_LAUNCH(KID_BLOCK_DEQUANT, (k_block_dequant<T, E8M0>), dim3(g), dim3(kWG), 0, st, d_code + r * in->ld, in->ld,
                     (const void *)((const uint8_t *)d_scale + srow * in->ld_scale * (E8M0 ? 1 : 4)), in->ld_scale, (T *)d_x_out + r * ld_x, ld_x,
-                    (uint32_t)units, (uint32_t)in->cols, (uint32_t)nb, by_nb, tile, in->format);
+                    (uint32_t)units, (uint32_t)in->cols, (uint32_t)nb, by_nb, tile, (uint32_t)(r % kBlk), in->format);
         LAUNCH_CHECK();
       }
       return RANS_OK;
@@ -169,7 +169,7 @@ namespace {
 
 int check_norm(const rans_norm_params *p) {
   if (!p) return RANS_ERR_ARG;
-  if (p->dtype > RANS_BF16 || p->weight_dtype > RANS_BF16) return RANS_ERR_ARG;
+  if (p->dtype > RANS_BF16 || p->weight_dtype > RANS_BF16 || p->reserved) return RANS_ERR_ARG;
   if (p->rows > kBlkMaxDim || p->cols < 1 || p->cols > kBlkMaxDim || !(p->eps >= 0) || !std::isfinite(p->eps)) return RANS_ERR_ARG;
   const uint64_t lds[4] = {p->ld_x, p->ld_res, p->ld_sum, p->ld_y};
   for (uint64_t ld : lds) {
@@ -334,6 +334,8 @@ int check_matmul(const rans_blocks *a, const rans_blocks *b) {
   return RANS_OK;
 }
 
+constexpr uint64_t kMatmulSlice = 1u << 17;  // rows of A and of B in a launch: 2^22 of the smallest tiles; whole tiles of scales
+
 }  // namespace
 
 extern "C" {
@@ -362,10 +364,22 @@ int rans_block_matmul(const uint8_t *d_a, const void *d_a_scale, const rans_bloc
   hipStream_t st = (hipStream_t)stream;
   const StreamDevice on(st);
   if (!on.ok) return RANS_ERR_HIP;
-  MatmulArgs p{d_a, d_b, d_a_scale, d_b_scale, d_c, a->ld, b->ld, a->ld_scale, b->ld_scale, ld_c, (uint32_t)a->rows, (uint32_t)b->rows,
-               (uint32_t)a->cols, a->scale_type == RANS_SCALE_E8M0, b->block == RANS_BLOCK_TILE, out_dtype};
   const int fmt = (a->format == RANS_E5M2 ? 2 : 0) + (b->format == RANS_E5M2 ? 1 : 0);
-  return out_dtype == RANS_F32 ? launch_matmul_wide(p, fmt, st) : launch_matmul_narrow(p, fmt, st);
+  const uint64_t sb = a->scale_type == RANS_SCALE_E8M0 ? 1 : 4;
+  for (uint64_t m = 0; m < a->rows; m += kMatmulSlice)
+    for (uint64_t n = 0; n < b->rows; n += kMatmulSlice) {
+      const uint64_t nm = a->rows - m < kMatmulSlice ? a->rows - m : kMatmulSlice, nn = b->rows - n < kMatmulSlice ? b->rows - n : kMatmulSlice;
+      MatmulArgs p{};
+      p.a = d_a + m * a->ld, p.lda = a->ld, p.sa = (const uint8_t *)d_a_scale + m * a->ld_scale * sb, p.ldsa = a->ld_scale;
+      p.b = d_b + n * b->ld, p.ldb = b->ld, p.ldsb = b->ld_scale;
+      p.sb = (const uint8_t *)d_b_scale + (b->block == RANS_BLOCK_TILE ? n / kBlk : n) * b->ld_scale * sb;
+      p.c = (uint8_t *)d_c + (m * ld_c + n) * eb, p.ldc = ld_c;
+      p.m = (uint32_t)nm, p.n = (uint32_t)nn, p.k = (uint32_t)a->cols;
+      p.e8m0 = a->scale_type == RANS_SCALE_E8M0, p.b_tile = b->block == RANS_BLOCK_TILE, p.out = out_dtype;
+      rc = out_dtype == RANS_F32 ? launch_matmul_wide(p, fmt, st) : launch_matmul_narrow(p, fmt, st);
+      if (rc) return rc;
+    }
+  return RANS_OK;
 }
 
 }  // extern "C"

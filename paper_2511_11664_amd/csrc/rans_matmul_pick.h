@@ -5,8 +5,6 @@
 
 namespace {
 
-constexpr uint64_t kMmMaxTiles = 1u << 22;  // work-groups of a launch
-
 typedef MmTile<2, 4, 8, 4, 2> MmLarge;   // 256 x 256, eight waves
 typedef MmTile<2, 4, 4, 2, 2> MmMedium;  // 128 x 128, eight waves
 typedef MmTile<2, 2, 4, 4, 2> MmWide;    // 128 x 128, four waves: widened operands, and operands of any alignment
@@ -15,18 +13,16 @@ typedef MmTile<2, 2, 2, 2, 4> MmSmall;   // 64 x 64, four waves, four stages
 template <typename TILE> uint64_t mm_tiles(const MatmulArgs &p) { return ((p.m + TILE::bm - 1) / TILE::bm) * (uint64_t)((p.n + TILE::bn - 1) / TILE::bn); }
 
 template <typename TILE, int FA, int FB, int SCALE, bool EXACT> int launch_tiles(const MatmulArgs &p, hipStream_t st) {
-  const uint64_t tiles_m = (p.m + TILE::bm - 1) / TILE::bm, tiles_n = (p.n + TILE::bn - 1) / TILE::bn;
-  if (tiles_m * tiles_n > kMmMaxTiles) return RANS_ERR_ARG;
-  PROF_LAUNCH(KID_BLOCK_MATMUL, (k_block_matmul<TILE, FA, FB, SCALE, EXACT>), dim3((uint32_t)(tiles_m * tiles_n)), dim3(TILE::threads), 0, st, p,
-              (uint32_t)tiles_m, (uint32_t)tiles_n);
+  const uint32_t tiles_m = (p.m + TILE::bm - 1) / TILE::bm, tiles_n = (p.n + TILE::bn - 1) / TILE::bn;
+  PROF_LAUNCH(KID_BLOCK_MATMUL, (k_block_matmul<TILE, FA, FB, SCALE, EXACT>), dim3(tiles_m * tiles_n), dim3(TILE::threads), 0, st, p, tiles_m,
+              tiles_n);
   LAUNCH_CHECK();
   return RANS_OK;
 }
 template <typename TILE, int FA, int FB, int SCALE, bool EXACT> int launch_any(const MatmulArgs &p, hipStream_t st) {
-  const uint64_t tiles_m = (p.m + TILE::bm - 1) / TILE::bm, tiles_n = (p.n + TILE::bn - 1) / TILE::bn;
-  if (tiles_m * tiles_n > kMmMaxTiles) return RANS_ERR_ARG;
-  PROF_LAUNCH(KID_BLOCK_MATMUL_ANY, (k_block_matmul_any<TILE, FA, FB, SCALE, EXACT>), dim3((uint32_t)(tiles_m * tiles_n)), dim3(TILE::threads), 0, st, p,
-              (uint32_t)tiles_m, (uint32_t)tiles_n);
+  const uint32_t tiles_m = (p.m + TILE::bm - 1) / TILE::bm, tiles_n = (p.n + TILE::bn - 1) / TILE::bn;
+  PROF_LAUNCH(KID_BLOCK_MATMUL_ANY, (k_block_matmul_any<TILE, FA, FB, SCALE, EXACT>), dim3(tiles_m * tiles_n), dim3(TILE::threads), 0, st, p, tiles_m,
+              tiles_n);
   LAUNCH_CHECK();
   return RANS_OK;
 }
@@ -51,7 +47,7 @@ inline double mm_cost_small(const MatmulArgs &p, uint32_t units) { return mm_cos
 // `tiles` is what the tile kernel would take for a block.  1 / 16 / 32 rows, K = 4096, us, few rows over 64 x 64 tiles:
 // 4096 rows of B 4.4 / 6.5 / 9.4 over 12, 12288 rows of B 9.6 / 15.3 / 24.7 over 13.
 inline bool mm_few(const MatmulArgs &p, double tiles) {
-  if (p.m > 32 || p.n > kMmMaxTiles * 16) return false;
+  if (p.m > 32) return false;
   const double bytes = (double)p.n * p.k * (1 + p.m / 16.0), nb = (p.k + kBlk - 1) / kBlk;
   return 2.6 + bytes / 7.9e6 < 1 + tiles * nb;
 }

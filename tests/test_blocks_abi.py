@@ -21,8 +21,11 @@ def lib():
 
 def blocks(rows=4, cols=256, **kw):
     base = dict(ld=256, ld_scale=4, format=0, scale_type=0, block=0)
+    reserved = kw.pop("reserved", 0)
     base.update(kw)
-    return B.make_blocks(rows, cols, **base)
+    b = B.make_blocks(rows, cols, **base)
+    b.reserved = reserved
+    return b
 
 
 def test_struct_layouts_match_header():
@@ -38,7 +41,7 @@ def test_default_leading_dimensions():
 
 @pytest.mark.parametrize("change, code", [
     (dict(ld=255), B.ERR_SHAPE), (dict(ld_scale=1), B.ERR_SHAPE), (dict(format=2), B.ERR_ARG), (dict(scale_type=2), B.ERR_ARG),
-    (dict(block=2), B.ERR_ARG), (dict(rows=(1 << 30) + 1), B.ERR_ARG), (dict(ld=(1 << 32) + 1), B.ERR_ARG)])
+    (dict(block=2), B.ERR_ARG), (dict(reserved=1), B.ERR_ARG), (dict(rows=(1 << 30) + 1), B.ERR_ARG), (dict(ld=(1 << 32) + 1), B.ERR_ARG)])
 def test_layouts_refused(lib, change, code):
     b = blocks(**change)
     assert lib.rans_block_quantize(FAKE, 256, B.F32, 0, FAKE, FAKE, b, None) == code
@@ -144,7 +147,9 @@ def test_binding_refuses_host_tensors_and_short_memory(lib):
     assert B.rans_norm_quantize(x, None, None, norm_params(dtype=B.F32, weight_dtype=B.F32), None, None, x, None, None, None) == B.ERR_ARG
     assert B.rans_norm_backward(x, None, x, None, x[0], norm_params(dtype=B.F32, weight_dtype=B.F32), x, None, None) == B.ERR_ARG
     assert B.rans_block_matmul(code, scale, b, code, scale, b, B.F32, x, 256, None) == B.ERR_ARG
-    assert B._holds(x, 4, 256, 256) and not B._holds(x, 4, 256, 257) and not B._holds(x, 5, 1, 256) and B._holds(x[:, :7], 4, 7, 256)
+    assert B._holds(x, 4, 256, 256, 4) and not B._holds(x, 4, 256, 257, 4) and not B._holds(x, 5, 1, 256, 4) and B._holds(x[:, :7], 4, 7, 256, 4)
+    assert not B._holds(x, 4, 256, 256, 2)                              # elements of another size
+    assert not B._holds(x[0].expand(8, 256), 8, 256, 256, 4)            # one row of memory, seen eight times
     assert not B._holds_blocks(code, scale, blocks(rows=5)) and B._holds_blocks(code, scale[:1], blocks(block=1))
     with pytest.raises(B.RansError):
         B._ld(x.t())

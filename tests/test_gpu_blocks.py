@@ -195,3 +195,15 @@ def test_many_short_rows():
         assert torch.equal(m.scale.reshape(-1)[:nb] if transpose else m.scale[:, 0], top)
         got = (m.code[0, :rows] if transpose else m.code[:, 0]).contiguous().view(torch.float8_e4m3fn).float()
         assert torch.equal(got, (x[:, 0] * (1 / top).repeat_interleave(128)[:rows]).to(torch.float8_e4m3fn).float())
+
+
+def test_rows_of_more_than_two_to_the_28():
+    """A launch holds fewer rows of these than a tile."""
+    cols = (1 << 28) + 200
+    for tile in (False, True):
+        x = (torch.arange(cols, device="cuda") % 255 - 127).to(torch.bfloat16).repeat(2, 1)
+        x[1] *= 2
+        m = B.BlockMatrix(2, cols, scale_type=B.SCALE_E8M0, block=B.BLOCK_TILE if tile else B.BLOCK_ROW).quantize(x)
+        y = m.dequantize(torch.empty_like(x))
+        # half a step of four bits at the value, or of the smallest codes at the block's scale, at most 1 / 128 here
+        assert ((y.float() - x.float()).abs() <= x.float().abs() / 16 + 1 / 128).all()

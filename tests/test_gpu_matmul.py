@@ -183,3 +183,18 @@ def test_matmul_binary32_results_keep_binary32():
     av, bv = (O.decode8(m.code[:, :2048].cpu(), 0) * O.spread(m.scale.cpu().double(), 200, 2048, False) for m in (a, b))
     want = av @ bv.t()
     assert ((c - want).norm() / want.norm()).item() <= 2.0 ** -19
+
+
+@pytest.mark.parametrize("out", (torch.float32, torch.bfloat16))
+@pytest.mark.parametrize("tile", (False, True))
+def test_matmul_of_more_rows_than_a_launch(out, tile):
+    """Two launches along A, two along B."""
+    rows = (1 << 17) + 77
+    for m, n in ((rows, 3), (3, rows), (40, rows)):
+        a, b = coded(m, 160, 0, False, False, 1), coded(n, 160, 0, False, tile, 2)
+        check(product(a, b, out), a, b, out, (m, n))
+
+
+def test_workspace_may_be_absent():
+    a, b = B.make_blocks(300, 512), B.make_blocks(200, 512)
+    assert B.rans_matmul_workspace_bytes(a, b) == (0, 0)
