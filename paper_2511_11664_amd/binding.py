@@ -317,16 +317,11 @@ def _at(t):
 
 
 def _holds(t, rows, cols, ld, size):
-    """Whether a tensor has elements of `size` bytes and its memory reaches to the end of rows x cols of them that are ld
-    apart; an absent one does."""
-    if t is None:
+    """Whether a tensor's memory reaches to the end of rows x cols elements of `size` bytes that are ld apart; an absent one does."""
+    if t is None or not rows or not cols:
         return True
-    if t.element_size() != size:
-        return False
-    if not rows or not cols:
-        return True
-    need = (rows - 1) * ld + cols
-    return need <= (t.numel() if t.is_contiguous() else _reach(t))
+    need = ((rows - 1) * ld + cols) * size
+    return need <= t.nbytes if t.is_contiguous() else need <= _reach(t) * t.element_size()
 
 
 def _reach(t):
@@ -341,7 +336,9 @@ def _reach(t):
 
 def _holds_blocks(code, scale, b):
     rows, cols = b.rows, b.cols
-    return _holds(code, rows, cols, b.ld, 1) and _holds(scale, -(-rows // BLOCK) if b.block else rows, -(-cols // BLOCK), b.ld_scale,
+    if not rows or not cols:
+        return True
+    return _holds(code, rows, cols, b.ld, 1) and _holds(scale, (rows + BLOCK - 1) // BLOCK if b.block else rows, (cols + BLOCK - 1) // BLOCK, b.ld_scale,
                                                         1 if b.scale_type else 4)
 
 

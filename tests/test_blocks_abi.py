@@ -135,7 +135,9 @@ def test_matmul_arguments_refused(lib):
     assert f(None, None, blocks(rows=0), None, None, b, B.BF16, None, 8, None, 0, None) in (B.ERR_ARG, B.OK)
     size = C.c_size_t()
     assert lib.rans_matmul_workspace_bytes(a, b, None) == B.ERR_ARG
-    assert lib.rans_matmul_workspace_bytes(a, b, C.byref(size)) == B.OK
+    assert lib.rans_matmul_workspace_bytes(a, b, C.byref(size)) == B.OK and size.value == 0
+    long = blocks(rows=64, cols=8192, ld=8192, ld_scale=64)
+    assert lib.rans_matmul_workspace_bytes(long, long, C.byref(size)) == B.OK and size.value >= 2 * 64 * 64 * 4
 
 
 def test_binding_refuses_host_tensors_and_short_memory(lib):
@@ -148,7 +150,7 @@ def test_binding_refuses_host_tensors_and_short_memory(lib):
     assert B.rans_norm_backward(x, None, x, None, x[0], norm_params(dtype=B.F32, weight_dtype=B.F32), x, None, None) == B.ERR_ARG
     assert B.rans_block_matmul(code, scale, b, code, scale, b, B.F32, x, 256, None) == B.ERR_ARG
     assert B._holds(x, 4, 256, 256, 4) and not B._holds(x, 4, 256, 257, 4) and not B._holds(x, 5, 1, 256, 4) and B._holds(x[:, :7], 4, 7, 256, 4)
-    assert not B._holds(x, 4, 256, 256, 2)                              # elements of another size
+    assert not B._holds(x.half(), 4, 256, 256, 4)                       # elements of half the size
     assert not B._holds(x[0].expand(8, 256), 8, 256, 256, 4)            # one row of memory, seen eight times
     assert not B._holds_blocks(code, scale, blocks(rows=5)) and B._holds_blocks(code, scale[:1], blocks(block=1))
     with pytest.raises(B.RansError):
