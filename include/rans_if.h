@@ -207,10 +207,11 @@ int rans_search_reshape(const uint8_t *d_sym, uint64_t n_elems, uint32_t q_bits,
  *
  * These entry points propagate NaN and infinities as floating-point arithmetic does; there is no data-dependent error
  * and nothing to read with rans_last_status().  ld and ld_scale may be anything from the row's length up to 2^32, rows and
- * cols 0 to 2^30.  Codes whose rows start on 16 bytes (d_code aligned, ld a multiple of 16) and tensors whose rows do are
- * faster; none is refused for its alignment beyond its element's.  Nothing outside the described rows and columns is read
- * or written.  Work goes to the device of `stream`.  A workspace needs no initialisation, and calls that may run at the
- * same time (two streams, two graphs) need one each. */
+ * cols 0 to 2^30.  None is refused for its alignment beyond its element's; the product of more than a few rows is faster
+ * where both matrices' rows of codes start on 16 bytes (d_code aligned, ld a multiple of 16).  Nothing outside the described
+ * rows and columns is read or written, and but for rans_norm_*, as said there, outputs do not overlap inputs.  Work goes to
+ * the device of `stream`.  A workspace is aligned to 256 bytes and needs no initialisation, and calls that may run at the
+ * same time (two streams, two graphs) need one each.  The same call gives the same bits every time. */
 enum { RANS_E4M3 = 0, RANS_E5M2 = 1 };
 enum { RANS_SCALE_F32 = 0, RANS_SCALE_E8M0 = 1 };
 enum { RANS_BLOCK_ROW = 0, RANS_BLOCK_TILE = 1 };
@@ -265,8 +266,9 @@ int rans_norm_backward(const void *d_dy, const void *d_dsum, const void *d_sum, 
  * d_c: a->rows x b->rows elements of out_dtype, ld_c elements from a row to the next; cols = 0 gives zeros.  The products of
  * a block are added on the matrix cores, its sum times both scales (whose binary32 product is taken first) is added in
  * binary32.  Results of 16 bits go through the 8-bit instructions, binary32 results through the bf16 ones, whose sums
- * keep all of binary32 (the 8-bit ones cut off what is about 2^-13 below the largest of their products and less).
- * Workspace: rans_matmul_workspace_bytes() (may be 0: then d_ws may be NULL). */
+ * keep all of binary32 (the 8-bit ones cut off what is about 2^-13 below the largest of their products and less).  A long
+ * K of a small result is cut into parts, whose binary32 sums are added up in their order.
+ * Workspace: rans_matmul_workspace_bytes() (0 where K is in one part: then d_ws may be NULL). */
 int rans_matmul_workspace_bytes(const rans_blocks *a, const rans_blocks *b, size_t *ws_bytes);
 int rans_block_matmul(const uint8_t *d_a, const void *d_a_scale, const rans_blocks *a, const uint8_t *d_b,
                       const void *d_b_scale, const rans_blocks *b, uint32_t out_dtype, void *d_c, uint64_t ld_c, void *d_ws,

@@ -327,6 +327,29 @@ __device__ __forceinline__ void mm_step(const uint8_t *__restrict__ code, const 
     for (int j = 0; j < MT; j++) asm volatile("" : "+v"(acc[i][j]));
 }
 
+// The part of K that a work-group takes (blockIdx.y), as a product of its own.
+template <int SCALE> __device__ __forceinline__ void mm_part(MatmulArgs &p) {
+  const uint32_t z = blockIdx.y, k0 = z * p.part_blocks * kBlk, left = p.k - k0, most = p.part_blocks * kBlk;
+  p.a += k0;
+  p.b += k0;
+  p.sa = (const uint8_t *)p.sa + z * p.part_blocks * (SCALE == MM_E8M0 ? 1 : 4);
+  p.sb = (const uint8_t *)p.sb + z * p.part_blocks * (SCALE == MM_E8M0 ? 1 : 4);
+  p.c = (float *)p.c + z * (uint64_t)p.m * p.ldc;
+  p.k = left < most ? left : most;
+}
+
+// The parts' sums in their order, rounded once: four columns a lane.
+__global__ __launch_bounds__(kWG) void k_block_matmul_sum(MatmulArgs p, const float *__restrict__ part, uint32_t parts, uint64_t ld) {
+  const uint32_t n = (blockIdx.x * kWG + threadIdx.x) * 4;
+  const uint32_t m = blockIdx.y;
+  if (n >= p.n) return;
+  f32x4 v = {0, 0, 0, 0};
+  part += m * ld + n;
+#pragma unroll 8
+  for (uint32_t s = 0; s < parts; s++) v += *(const f32x4 *)(part + s * p.m * ld);
+  store_c4(p, m, n, v);
+}
+
 // A wave's results of a tile.
 template <typename TILE> __device__ __forceinline__ void mm_store(const MatmulArgs &p, uint32_t m0, uint32_t n0, uint32_t wm, uint32_t wn, uint32_t lane, const f32x4 (&acc)[TILE::nt][TILE::mt]) {
   constexpr int NT = TILE::nt, MT = TILE::mt;
@@ -399,6 +422,7 @@ template <typename TILE, int SCALE> struct MmRegs {
 // Operands of any alignment: two stages, the next block in registers while this one's products run.
 template <typename TILE, int FA, int FB, int SCALE, bool EXACT>
 __global__ __launch_bounds__(TILE::threads, 2) void k_block_matmul_any(MatmulArgs p, uint32_t tiles_m, uint32_t tiles_n) {
+  if (p.part_blocks) mm_part<SCALE>(p);
   __shared__ __attribute__((aligned(16))) uint8_t s_code[2][TILE::rows * kBlk];
   __shared__ __attribute__((aligned(16))) uint32_t s_scale[2][TILE::rows * (SCALE == MM_E8M0 ? 1 : TILE::stages)];
   const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave % TILE::wm, wn = wave / TILE::wm;
@@ -454,6 +478,7 @@ __global__ __launch_bounds__(TILE::threads, 2) void k_block_matmul(MatmulArgs p,
   constexpr int LA = BM * 8 / NTH, LB = BN * 8 / NTH, SROWS = (ROWS + NTH - 1) / NTH;
   constexpr uint32_t SB = SCALE == MM_E8M0 ? 1 : 4;  // bytes of a scale
   static_assert(S == 2 || S == 4, "scales are loaded as two or four");
+  if (p.part_blocks) mm_part<SCALE>(p);
   __shared__ __attribute__((aligned(1024))) uint8_t s_code0[ROWS * kBlk];
   __shared__ __attribute__((aligned(1024))) uint8_t s_code1[ROWS * kBlk];
   __shared__ __attribute__((aligned(1024))) uint8_t s_code2[S > 2 ? ROWS * kBlk : 16];

@@ -12,16 +12,18 @@ typedef MmTile<2, 2, 2, 2, 4> MmSmall;   // 64 x 64, four waves, four stages
 
 template <typename TILE> uint64_t mm_tiles(const MatmulArgs &p) { return ((p.m + TILE::bm - 1) / TILE::bm) * (uint64_t)((p.n + TILE::bn - 1) / TILE::bn); }
 
+inline uint32_t mm_parts_of(const MatmulArgs &p) { return p.part_blocks ? ((p.k + kBlk - 1) / kBlk + p.part_blocks - 1) / p.part_blocks : 1; }
+
 template <typename TILE, int FA, int FB, int SCALE, bool EXACT> int launch_tiles(const MatmulArgs &p, hipStream_t st) {
   const uint32_t tiles_m = (p.m + TILE::bm - 1) / TILE::bm, tiles_n = (p.n + TILE::bn - 1) / TILE::bn;
-  PROF_LAUNCH(KID_BLOCK_MATMUL, (k_block_matmul<TILE, FA, FB, SCALE, EXACT>), dim3(tiles_m * tiles_n), dim3(TILE::threads), 0, st, p, tiles_m,
+  PROF_LAUNCH(KID_BLOCK_MATMUL, (k_block_matmul<TILE, FA, FB, SCALE, EXACT>), dim3(tiles_m * tiles_n, mm_parts_of(p)), dim3(TILE::threads), 0, st, p, tiles_m,
               tiles_n);
   LAUNCH_CHECK();
   return RANS_OK;
 }
 template <typename TILE, int FA, int FB, int SCALE, bool EXACT> int launch_any(const MatmulArgs &p, hipStream_t st) {
   const uint32_t tiles_m = (p.m + TILE::bm - 1) / TILE::bm, tiles_n = (p.n + TILE::bn - 1) / TILE::bn;
-  PROF_LAUNCH(KID_BLOCK_MATMUL_ANY, (k_block_matmul_any<TILE, FA, FB, SCALE, EXACT>), dim3(tiles_m * tiles_n), dim3(TILE::threads), 0, st, p, tiles_m,
+  PROF_LAUNCH(KID_BLOCK_MATMUL_ANY, (k_block_matmul_any<TILE, FA, FB, SCALE, EXACT>), dim3(tiles_m * tiles_n, mm_parts_of(p)), dim3(TILE::threads), 0, st, p, tiles_m,
               tiles_n);
   LAUNCH_CHECK();
   return RANS_OK;
@@ -53,6 +55,18 @@ inline bool mm_few(const MatmulArgs &p, double tiles) {
 }
 inline bool mm_fetch_fits(const MatmulArgs &p) {
   return aligned_to(p.a, 16) && aligned_to(p.b, 16) && p.lda % 16 == 0 && p.ldb % 16 == 0 && p.lda <= kMmMaxLd && p.ldb <= kMmMaxLd;
+}
+
+// The product with its K in parts: `go` launches the tiles, whose sums then become the result.
+template <typename F> int in_parts(const MatmulArgs &p, MatmulParts parts, void *ws, hipStream_t st, F go) {
+  if (parts.n < 2) return go(p);
+  MatmulArgs q = p;
+  q.c = ws, q.ldc = matmul_part_ld(p.n), q.out = RANS_F32, q.part_blocks = parts.blocks;
+  const int rc = go(q);
+  if (rc) return rc;
+  PROF_LAUNCH(KID_BLOCK_MATMUL_SUM, k_block_matmul_sum, dim3((p.n + 4 * kWG - 1) / (4 * kWG), p.m), dim3(kWG), 0, st, p, (const float *)ws, parts.n, q.ldc);
+  LAUNCH_CHECK();
+  return RANS_OK;
 }
 
 template <typename F> int by_format(int fmt, F f) {

@@ -14,18 +14,21 @@
 #include "rans_matmul.h"
 #include "rans_matmul_pick.h"
 
-int launch_matmul_wide(const MatmulArgs &p, int fmt, hipStream_t st) {
+int launch_matmul_wide(const MatmulArgs &p, int fmt, void *ws, hipStream_t st) {
   const uint32_t units = compute_units() ? compute_units() : 256;
   const double medium = mm_cost_medium(p, units), small = mm_cost_small(p, units);
   const bool few = mm_few(p, small), fetch = mm_fetch_fits(p);
+  const MatmulParts parts = matmul_parts(p.m, p.n, p.k);
   return by_format(fmt, [&](auto fa, auto fb) {
     return by_scale(p, [&](auto scale) {
       constexpr int FA = decltype(fa)::value, FB = decltype(fb)::value, SCALE = decltype(scale)::value;
       if (few && p.m <= 16) return launch_few<1, 4, 8, FA, FB, SCALE, true>(p, st);
       if (few) return launch_few<2, 8, 4, FA, FB, SCALE, true>(p, st);
-      if (!fetch) return launch_any<MmWide, FA, FB, SCALE, true>(p, st);
-      if (small <= medium) return launch_tiles<MmSmall, FA, FB, SCALE, true>(p, st);
-      return launch_tiles<MmWide, FA, FB, SCALE, true>(p, st);
+      return in_parts(p, parts, ws, st, [&](const MatmulArgs &q) {
+        if (!fetch) return launch_any<MmWide, FA, FB, SCALE, true>(q, st);
+        if (parts.n > 1 || small <= medium) return launch_tiles<MmSmall, FA, FB, SCALE, true>(q, st);
+        return launch_tiles<MmWide, FA, FB, SCALE, true>(q, st);
+      });
     });
   });
 }
