@@ -28,7 +28,7 @@ int launch_matmul_narrow(const MatmulArgs &p, int fmt, void *ws, hipStream_t st)
       if (few && p.m <= 16) return launch_few<1, 4, 8, FA, FB, SCALE, false>(p, st);
       if (few) return launch_few<2, 8, 4, FA, FB, SCALE, false>(p, st);
       return in_parts(p, parts, ws, st, [&](const MatmulArgs &q) {
-        if (!fetch) return launch_any<MmWide, FA, FB, SCALE, false>(q, st);
+        if (!fetch) return parts.n > 1 || small <= medium ? launch_any<MmSmall, FA, FB, SCALE, false>(q, st) : launch_any<MmWide, FA, FB, SCALE, false>(q, st);
         if constexpr (FB == 0) {
           if (parts.n > 1 || (small <= medium && (small <= large || SCALE == MM_F32_ROW))) return launch_tiles<MmSmall, FA, FB, SCALE, false>(q, st);
           if constexpr (SCALE != MM_F32_ROW)

@@ -8,6 +8,7 @@ namespace {
 typedef MmTile<2, 4, 8, 4, 2> MmLarge;   // 256 x 256, eight waves
 typedef MmTile<2, 4, 4, 2, 2> MmMedium;  // 128 x 128, eight waves
 typedef MmTile<2, 2, 4, 4, 2> MmWide;    // 128 x 128, four waves: widened operands, and operands of any alignment
+typedef MmTile<4, 2, 4, 4, 2> MmBroad;   // 128 rows of A x 256, eight waves: both, scales of each row of B (4096 x 4096 x 4096 224 -> 173 us)
 typedef MmTile<2, 2, 2, 2, 4> MmSmall;   // 64 x 64, four waves, four stages
 
 template <typename TILE> uint64_t mm_tiles(const MatmulArgs &p) { return ((p.m + TILE::bm - 1) / TILE::bm) * (uint64_t)((p.n + TILE::bn - 1) / TILE::bn); }
@@ -35,7 +36,9 @@ template <int MT, int W, int AHEAD, int FA, int FB, int SCALE, bool EXACT> int l
 }
 
 // Rounds of work-groups times what a round takes, us a block: `alone` with one work-group on a compute unit, `both` with two
-// (K = 4096, 256 units; 48 to 1024 rows of A, 1024 to 12288 of B).
+// (K = 4096, 256 units; 48 to 1024 rows of A, 1024 to 12288 of B).  Widened operands and operands of any alignment take
+// longer, but change between 64 x 64 and 128 x 128 tiles at the same sizes.  K = 4096, 64 x 64 / larger, us: 395 x 4096
+// widened 27 / 43, any alignment 31 / 40, both 39 / 84; 2048 x 4096 103 / 76, 88 / 57, 116 / 88.
 inline double mm_cost(uint64_t tiles, uint32_t units, double alone, double both) {
   const uint64_t slots = both > 0 ? 2ull * units : units, whole = tiles / slots, rest = tiles % slots;
   const double full = both > 0 ? both : alone;

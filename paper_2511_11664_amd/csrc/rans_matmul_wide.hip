@@ -25,8 +25,8 @@ int launch_matmul_wide(const MatmulArgs &p, int fmt, void *ws, hipStream_t st) {
       if (few && p.m <= 16) return launch_few<1, 4, 8, FA, FB, SCALE, true>(p, st);
       if (few) return launch_few<2, 8, 4, FA, FB, SCALE, true>(p, st);
       return in_parts(p, parts, ws, st, [&](const MatmulArgs &q) {
-        if (!fetch) return launch_any<MmWide, FA, FB, SCALE, true>(q, st);
-        if (parts.n > 1 || small <= medium) return launch_tiles<MmSmall, FA, FB, SCALE, true>(q, st);
+        if (parts.n > 1 || small <= medium) return fetch ? launch_tiles<MmSmall, FA, FB, SCALE, true>(q, st) : launch_any<MmSmall, FA, FB, SCALE, true>(q, st);
+        if (!fetch) return launch_any<std::conditional_t<SCALE == MM_F32_TILE, MmWide, MmBroad>, FA, FB, SCALE, true>(q, st);
         return launch_tiles<MmWide, FA, FB, SCALE, true>(q, st);
       });
     });
