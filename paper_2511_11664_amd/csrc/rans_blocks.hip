@@ -196,18 +196,22 @@ template <typename F> int by_row_forward(const rans_norm_params &p, F f) {
 }
 
 // Backward, and its work-groups, which are the rows of partial sums too: one or two on a compute unit, since the next row's
-// loads are under way anyway and each partial row is written and read again.  16384 x 4096 with 256 / 512 of them 88.8 /
-// 95.6 us; 16384 x 2048 (256 threads each) 59.7 / 45.6; 395 x 5120 (1024 threads) 8.8, with one for every row 12.5.
+// loads are under way anyway and each partial row is written and read again; no more than take the same number of rows each.
+// 16384 x 4096 with 256 / 512 of them 85.5 / 88.3 us; 16384 x 2048 (256 threads each) 59.7 / 45.6; 395 x 5120 with 198 /
+// 256 / 395 of them 9.3 / 9.8 / 11.4, and with 1024 threads each instead of 640 10.1 / 10.5 / 13.6.
 template <typename F> int by_row_backward(const rans_norm_params &p, F f) {
   if (p.cols <= 64 * 8) return with_row<64, 1>(f);
   if (p.cols <= 256 * 8) return with_row<256, 1>(f);
   if (p.cols <= 512 * 8) return with_row<512, 1>(f);
+  if (p.cols <= 640 * 8) return with_row<640, 1>(f);
   if (p.cols <= 1024 * 8) return with_row<1024, 1>(f);
   return with_row<512, 0>(f);
 }
 uint32_t norm_parts(const rans_norm_params &p) {
   const uint32_t most = p.cols <= 64 * 8 ? 2048 : p.cols <= 256 * 8 ? 512 : 256;
-  return (uint32_t)(p.rows < most ? p.rows : most);
+  if (p.rows <= most) return (uint32_t)p.rows;
+  const uint64_t each = (p.rows + most - 1) / most;
+  return (uint32_t)((p.rows + each - 1) / each);
 }
 
 }  // namespace

@@ -208,9 +208,7 @@ __global__ __launch_bounds__(NT) void k_norm_bwd(NormBwd a) {
 #pragma unroll
       for (int k = 0; k < NV; k++) {
         const uint32_t c = (k * NT + t) * 8;
-#pragma unroll
-        for (int i = 0; i < 8; i++)
-          if (c + i < n) part[c + i] = dw[k][i];
+        if (c < n) store8(part, c, n, dw[k]);
       }
     }
   } else {

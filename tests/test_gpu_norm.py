@@ -154,7 +154,7 @@ def check_backward(rows, cols, dtype, dy, dsum, h, w, rstd, dx, dw):
 @pytest.mark.parametrize("wide_weight", (False, True))
 @pytest.mark.parametrize("dtype", tuple(CODE))
 def test_norm_backward(dtype, wide_weight):
-    for i, (rows, cols) in enumerate(SHAPES + [(1500, 200), (600, 9000)]):
+    for i, (rows, cols) in enumerate(SHAPES + [(1500, 200), (600, 9000), (395, 4500)]):
         dy, ds, h, w, rstd = bwd_data(rows, cols, dtype, wide_weight)
         ds = None if i % 4 == 1 else ds
         ld, off = (cols + 3, 1) if i % 3 == 2 else (cols, 0)
