@@ -210,7 +210,7 @@ int rans_search_reshape(const uint8_t *d_sym, uint64_t n_elems, uint32_t q_bits,
  * cols 0 to 2^30.  None is refused for its alignment beyond its element's; the product of more than a few rows is faster
  * where both matrices' rows of codes start on 16 bytes (d_code aligned, ld a multiple of 16).  Nothing outside the described
  * rows and columns is read or written, and but for rans_norm_*, as said there, outputs do not overlap inputs.  Work goes to
- * the device of `stream`.  A workspace is aligned to 256 bytes and needs no initialisation, and calls that may run at the
+ * the device of `stream` (the current device where that is NULL).  A workspace is aligned to 256 bytes and needs no initialisation, and calls that may run at the
  * same time (two streams, two graphs) need one each.  The same call gives the same bits every time. */
 enum { RANS_E4M3 = 0, RANS_E5M2 = 1 };
 enum { RANS_SCALE_F32 = 0, RANS_SCALE_E8M0 = 1 };
@@ -242,7 +242,7 @@ int rans_block_dequantize(const uint8_t *d_code, const void *d_scale, const rans
  * each row by itself.  x, residual, sum, y: rows x cols elements of dtype, ld_* elements from a row to the next; weight:
  * cols elements of dtype or binary32.  d_res, d_weight (all ones) and each of the outputs d_sum (h), d_rstd (binary32, one
  * a row, for rans_norm_backward), d_y (y rounded to dtype) and d_code / d_scale (y coded as `out` says, RANS_BLOCK_ROW)
- * may be NULL.  Outputs may be an input's own memory (same pointer, same ld). */
+ * may be NULL.  d_sum and d_y may be d_x's or d_res's own memory (same pointer, same ld).  Every ld_* is at least cols. */
 typedef struct {
   uint64_t rows, cols;  /* cols >= 1 */
   uint64_t ld_x, ld_res, ld_sum, ld_y;

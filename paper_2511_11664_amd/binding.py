@@ -298,18 +298,29 @@ def workspace(ws_bytes: int, device="cuda") -> torch.Tensor:
     return t[off:off + ws_bytes]
 
 
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # the current stream's handle without a Stream object
+# the current device, and the handle of the current stream on a device without a Stream object
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
 def _on(first, *more):
-    """The current stream's handle on the first tensor's device, None where a tensor is in host memory or on another device."""
+    """The first tensor's device, None where a tensor is in host memory or on another device."""
     dev = first.get_device()
     if dev < 0:
         return None
     for t in more:
         if t is not None and t.get_device() != dev:
             return None
-    return _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream(dev).cuda_stream
+    return dev
+
+
+def _enqueue(entry, dev, *args):
+    """entry(*args, the current stream on `dev`).  Every device's default stream has the same handle, which stands for the
+    current device's: that is `dev` for the call."""
+    if _current_device() == dev:
+        return entry(*args, _raw_stream(dev))
+    with torch.cuda.device(dev):
+        return entry(*args, _raw_stream(dev))
 
 
 def _at(t):
@@ -320,8 +331,12 @@ def _holds(t, rows, cols, ld, size):
     """Whether a tensor's memory reaches to the end of rows x cols elements of `size` bytes that are ld apart; an absent one does."""
     if t is None or not rows or not cols:
         return True
-    need = ((rows - 1) * ld + cols) * size
-    return need <= t.nbytes if t.is_contiguous() else need <= _reach(t) * t.element_size()
+    return ((rows - 1) * ld + cols) * size <= _bytes(t)
+
+
+def _bytes(t):
+    """Bytes of memory from a tensor's first element on that it has for sure."""
+    return 0 if t is None else t.nbytes if t.is_contiguous() else _reach(t) * t.element_size()
 
 
 def _reach(t):
@@ -347,29 +362,29 @@ def _size(dtype):
 
 
 def rans_block_quantize(d_x, ld_x, in_dtype, transpose, d_code, d_scale, out) -> int:
-    st = _on(d_x, d_code, d_scale)
-    if st is None or not _holds_blocks(d_code, d_scale, out) or not _holds(d_x, *((out.cols, out.rows) if transpose else (out.rows, out.cols)), ld_x,
+    dev = _on(d_x, d_code, d_scale)
+    if dev is None or not _holds_blocks(d_code, d_scale, out) or not _holds(d_x, *((out.cols, out.rows) if transpose else (out.rows, out.cols)), ld_x,
                                                                                  _size(in_dtype)):
         return ERR_ARG
-    return lib().rans_block_quantize(_at(d_x), ld_x, in_dtype, transpose, _at(d_code), _at(d_scale), out, st)
+    return _enqueue(lib().rans_block_quantize, dev, _at(d_x), ld_x, in_dtype, transpose, _at(d_code), _at(d_scale), out)
 
 
 def rans_block_dequantize(d_code, d_scale, blocks, out_dtype, d_x_out, ld_x) -> int:
-    st = _on(d_x_out, d_code, d_scale)
-    if st is None or not _holds_blocks(d_code, d_scale, blocks) or not _holds(d_x_out, blocks.rows, blocks.cols, ld_x, _size(out_dtype)):
+    dev = _on(d_x_out, d_code, d_scale)
+    if dev is None or not _holds_blocks(d_code, d_scale, blocks) or not _holds(d_x_out, blocks.rows, blocks.cols, ld_x, _size(out_dtype)):
         return ERR_ARG
-    return lib().rans_block_dequantize(_at(d_code), _at(d_scale), blocks, out_dtype, _at(d_x_out), ld_x, st)
+    return _enqueue(lib().rans_block_dequantize, dev, _at(d_code), _at(d_scale), blocks, out_dtype, _at(d_x_out), ld_x)
 
 
 def rans_norm_quantize(d_x, d_res, d_weight, p, d_sum, d_rstd, d_y, d_code, d_scale, out) -> int:
-    st = _on(d_x, d_res, d_weight, d_sum, d_rstd, d_y, d_code, d_scale)
+    dev = _on(d_x, d_res, d_weight, d_sum, d_rstd, d_y, d_code, d_scale)
     rows, cols, e = p.rows, p.cols, _size(p.dtype)
-    if st is None or not (_holds(d_x, rows, cols, p.ld_x, e) and _holds(d_res, rows, cols, p.ld_res, e) and _holds(d_sum, rows, cols, p.ld_sum, e)
+    if dev is None or not (_holds(d_x, rows, cols, p.ld_x, e) and _holds(d_res, rows, cols, p.ld_res, e) and _holds(d_sum, rows, cols, p.ld_sum, e)
                           and _holds(d_y, rows, cols, p.ld_y, e) and _holds(d_weight, 1, cols, cols, _size(p.weight_dtype))
                           and _holds(d_rstd, 1, rows, rows, 4)
                           and (d_code is None or (out is not None and _holds_blocks(d_code, d_scale, out)))):
         return ERR_ARG
-    return lib().rans_norm_quantize(_at(d_x), _at(d_res), _at(d_weight), p, _at(d_sum), _at(d_rstd), _at(d_y), _at(d_code), _at(d_scale), out, st)
+    return _enqueue(lib().rans_norm_quantize, dev, _at(d_x), _at(d_res), _at(d_weight), p, _at(d_sum), _at(d_rstd), _at(d_y), _at(d_code), _at(d_scale), out)
 
 
 def rans_norm_workspace_bytes(p: NormParams):
@@ -379,14 +394,14 @@ def rans_norm_workspace_bytes(p: NormParams):
 
 
 def rans_norm_backward(d_dy, d_dsum, d_sum, d_weight, d_rstd, p, d_dx, d_dweight, d_ws) -> int:
-    st = _on(d_dy, d_dsum, d_sum, d_weight, d_rstd, d_dx, d_dweight, d_ws)
+    dev = _on(d_dy, d_dsum, d_sum, d_weight, d_rstd, d_dx, d_dweight, d_ws)
     rows, cols, e = p.rows, p.cols, _size(p.dtype)
-    if st is None or not (_holds(d_dy, rows, cols, p.ld_y, e) and _holds(d_dsum, rows, cols, p.ld_res, e) and _holds(d_sum, rows, cols, p.ld_sum, e)
+    if dev is None or not (_holds(d_dy, rows, cols, p.ld_y, e) and _holds(d_dsum, rows, cols, p.ld_res, e) and _holds(d_sum, rows, cols, p.ld_sum, e)
                           and _holds(d_dx, rows, cols, p.ld_x, e) and _holds(d_weight, 1, cols, cols, _size(p.weight_dtype))
                           and _holds(d_rstd, 1, rows, rows, 4) and _holds(d_dweight, 1, cols, cols, 4)):
         return ERR_ARG
-    return lib().rans_norm_backward(_at(d_dy), _at(d_dsum), _at(d_sum), _at(d_weight), _at(d_rstd), p, _at(d_dx), _at(d_dweight), _at(d_ws),
-                                    0 if d_ws is None else d_ws.numel() * d_ws.element_size(), st)
+    return _enqueue(lib().rans_norm_backward, dev, _at(d_dy), _at(d_dsum), _at(d_sum), _at(d_weight), _at(d_rstd), p, _at(d_dx), _at(d_dweight), _at(d_ws),
+                    _bytes(d_ws))
 
 
 def rans_matmul_workspace_bytes(a: Blocks, b: Blocks):
@@ -396,11 +411,11 @@ def rans_matmul_workspace_bytes(a: Blocks, b: Blocks):
 
 
 def rans_block_matmul(d_a, d_a_scale, a, d_b, d_b_scale, b, out_dtype, d_c, ld_c, d_ws) -> int:
-    st = _on(d_c, d_a, d_a_scale, d_b, d_b_scale, d_ws)
-    if st is None or not (_holds_blocks(d_a, d_a_scale, a) and _holds_blocks(d_b, d_b_scale, b) and _holds(d_c, a.rows, b.rows, ld_c, _size(out_dtype))):
+    dev = _on(d_c, d_a, d_a_scale, d_b, d_b_scale, d_ws)
+    if dev is None or not (_holds_blocks(d_a, d_a_scale, a) and _holds_blocks(d_b, d_b_scale, b) and _holds(d_c, a.rows, b.rows, ld_c, _size(out_dtype))):
         return ERR_ARG
-    return lib().rans_block_matmul(_at(d_a), _at(d_a_scale), a, _at(d_b), _at(d_b_scale), b, out_dtype, _at(d_c), ld_c, _at(d_ws),
-                                   0 if d_ws is None else d_ws.numel() * d_ws.element_size(), st)
+    return _enqueue(lib().rans_block_matmul, dev, _at(d_a), _at(d_a_scale), a, _at(d_b), _at(d_b_scale), b, out_dtype, _at(d_c), ld_c, _at(d_ws),
+                    _bytes(d_ws))
 
 
 class BlockMatrix:

@@ -174,3 +174,31 @@ def test_oracle_scales_are_the_least_power_of_two(fmt):
     for i in range(a.shape[1]):
         s = O.block_scales(a[:1, i:i + 1], fmt, True, False).item()
         assert v * s >= a[0, i].item() > v * s / 2
+
+
+def test_calls_go_to_their_tensors_device(monkeypatch):
+    """Tensors of a device that is not the current one: the call is made with theirs as the current one, and the current one is put back."""
+    current, seen = [0], []
+
+    class Device:
+        def __init__(self, dev):
+            self.dev = dev
+
+        def __enter__(self):
+            self.before, current[0] = current[0], self.dev
+
+        def __exit__(self, *_):
+            current[0] = self.before
+
+    monkeypatch.setattr(B, "_current_device", lambda: current[0])
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(B, "_raw_stream", lambda dev: 100 + dev)
+    for dev in (0, 1):
+        assert B._enqueue(lambda *a: seen.append((current[0], a)) or 7, dev, "x", "y") == 7
+    assert seen == [(0, ("x", "y", 100)), (1, ("x", "y", 101))] and current == [0]
+
+
+def test_memory_of_a_workspace():
+    whole = torch.empty(4, 256, dtype=torch.float32)
+    assert B._bytes(None) == 0 and B._bytes(whole) == 4096 and B._bytes(whole[1:]) == 3072
+    assert B._bytes(torch.empty(1, dtype=torch.uint8).expand(4096)) == 1 and B._bytes(whole[:, :128]) == (3 * 256 + 128) * 4
