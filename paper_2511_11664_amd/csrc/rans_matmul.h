@@ -20,11 +20,20 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-// 16 codes of a row from k on, those from K on are zero.  Rows may start anywhere.
+// 16 codes of a row from k on, those from K on are zero.  Rows may start anywhere.  The 16 around the row's end are its last
+// 16, moved down (byte by byte is a trip to memory for each).
 __device__ inline u32x4 load_codes16(const uint8_t *row, uint32_t k, uint32_t K) {
   u32x4 w = {0, 0, 0, 0};
   if (k + 16 <= K) {
     __builtin_memcpy(&w, row + k, 16);
+  } else if (K >= 16) {
+    if (k < K) {
+      uint64_t q[2];
+      __builtin_memcpy(q, row + K - 16, 16);
+      const uint32_t by = (k + 16 - K) * 8;  // 8 to 120 bits
+      const uint64_t lo = by < 64 ? q[0] >> by | q[1] << (64 - by) : q[1] >> (by - 64), hi = by < 64 ? q[1] >> by : 0;
+      w = (u32x4){(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+    }
   } else {
     for (uint32_t i = 0; i < 16; i++)
       if (k + i < K) w[i >> 2] |= (uint32_t)row[k + i] << (8 * (i & 3));
@@ -585,6 +594,8 @@ __global__ __launch_bounds__(TILE::threads, 2) void k_block_matmul(MatmulArgs p,
   }
   // fewer whole blocks than a round, then what is left of a row
   const uint32_t back = nb >= S && kb + S > nb ? kb + S - nb : 0;
+  MmRegs<TILE, SCALE, EXACT> q;
+  if (full < nb) q.load(p, m0, n0, full);
 #pragma unroll
   for (int s = 0; s < S - 1; s++)
     if (kb + s < full) {
@@ -593,8 +604,6 @@ __global__ __launch_bounds__(TILE::threads, 2) void k_block_matmul(MatmulArgs p,
     }
   sync(None{});
   if (full < nb) {
-    MmRegs<TILE, SCALE, EXACT> q;
-    q.load(p, m0, n0, full);
     q.put(s_code0);
     sync(None{});
     mm_step<TILE, FA, FB, SCALE, EXACT>(s_code0, s_scale[set], full % S + back, wm, wn, lane, acc);
