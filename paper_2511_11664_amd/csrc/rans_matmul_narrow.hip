@@ -20,7 +20,7 @@
 int launch_matmul_narrow(const MatmulArgs &p, int fmt, void *ws, hipStream_t st) {
   const uint32_t units = compute_units() ? compute_units() : 256;
   const double large = mm_cost_large(p, units), medium = mm_cost_medium(p, units), small = mm_cost_small(p, units);
-  const bool few = mm_few(p, small), fetch = mm_fetch_fits(p);
+  const bool few = mm_few(p, small), fetch = mm_fetch_fits(p), deep = mm_deep(p, units, 8);
   const MatmulParts parts = matmul_parts(p.m, p.n, p.k);
   return by_format(fmt, [&](auto fa, auto fb) {
     return by_scale(p, [&](auto scale) {
@@ -34,7 +34,7 @@ int launch_matmul_narrow(const MatmulArgs &p, int fmt, void *ws, hipStream_t st)
           if constexpr (SCALE != MM_F32_ROW)
             if (large < medium) return launch_tiles<MmLarge, FA, FB, SCALE, false>(q, st);
         }
-        return launch_tiles<MmMedium, FA, FB, SCALE, false>(q, st);
+        return deep ? launch_tiles<MmDeep, FA, FB, SCALE, false>(q, st) : launch_tiles<MmMedium, FA, FB, SCALE, false>(q, st);
       });
     });
   });

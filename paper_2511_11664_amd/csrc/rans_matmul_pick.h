@@ -7,6 +7,7 @@ namespace {
 
 typedef MmTile<2, 4, 8, 4, 2> MmLarge;   // 256 x 256, eight waves
 typedef MmTile<2, 4, 4, 2, 2> MmMedium;  // 128 x 128, eight waves
+typedef MmTile<2, 4, 4, 2, 4> MmDeep;    // the same with four stages, which leave room for one work-group on a compute unit
 typedef MmTile<2, 2, 4, 4, 2> MmWide;    // 128 x 128, four waves: widened operands, and operands of any alignment
 typedef MmTile<4, 2, 4, 4, 2> MmBroad;   // 128 rows of A x 256, eight waves: both, scales of each row of B (4096 x 4096 x 4096 224 -> 173 us)
 typedef MmTile<2, 2, 2, 2, 4> MmSmall;   // 64 x 64, four waves, four stages
@@ -47,6 +48,13 @@ inline double mm_cost(uint64_t tiles, uint32_t units, double alone, double both)
 inline double mm_cost_large(const MatmulArgs &p, uint32_t units) { return mm_cost(mm_tiles<MmLarge>(p), units, 1.6, 0); }
 inline double mm_cost_medium(const MatmulArgs &p, uint32_t units) { return mm_cost(mm_tiles<MmMedium>(p), units, 0.64, 1.1); }
 inline double mm_cost_small(const MatmulArgs &p, uint32_t units) { return mm_cost(mm_tiles<MmSmall>(p), units, 0.36, 0.5); }
+
+// Four stages where each 128 x 128 tile has a compute unit to itself anyway, and K lasts a few rounds of them.  1024 x 4096,
+// us, with two / four stages: K = 512 6.9 / 7.5, 4096 28.9 / 26.0 (powers of two 28.4 / 23.7), 12288 77.5 / 73.6 (82.5 / 71.7);
+// widened, over four waves with two stages, 12.2 / 11.9, 51.2 / 49.1, 136 / 131, and 700 x 4096 x 4096 47.7 / 44.5.
+inline bool mm_deep(const MatmulArgs &p, uint32_t units, uint32_t least_blocks) {
+  return mm_tiles<MmDeep>(p) <= units && p.k >= least_blocks * kBlk;
+}
 
 // Few rows of A: the kernel for them takes about 2.6 us and what B, and A once for every 16 rows of B, take at 7.9 MB a us;
 // `tiles` is what the tile kernel would take for a block.  1 / 16 / 32 rows, K = 4096, us, few rows over 64 x 64 tiles:

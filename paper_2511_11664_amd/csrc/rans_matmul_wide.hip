@@ -17,7 +17,7 @@
 int launch_matmul_wide(const MatmulArgs &p, int fmt, void *ws, hipStream_t st) {
   const uint32_t units = compute_units() ? compute_units() : 256;
   const double medium = mm_cost_medium(p, units), small = mm_cost_small(p, units);
-  const bool few = mm_few(p, small), fetch = mm_fetch_fits(p);
+  const bool few = mm_few(p, small), fetch = mm_fetch_fits(p), deep = mm_deep(p, units, 1);
   const MatmulParts parts = matmul_parts(p.m, p.n, p.k);
   return by_format(fmt, [&](auto fa, auto fb) {
     return by_scale(p, [&](auto scale) {
@@ -27,7 +27,7 @@ int launch_matmul_wide(const MatmulArgs &p, int fmt, void *ws, hipStream_t st) {
       return in_parts(p, parts, ws, st, [&](const MatmulArgs &q) {
         if (parts.n > 1 || small <= medium) return fetch ? launch_tiles<MmSmall, FA, FB, SCALE, true>(q, st) : launch_any<MmSmall, FA, FB, SCALE, true>(q, st);
         if (!fetch) return launch_any<std::conditional_t<SCALE == MM_F32_TILE, MmWide, MmBroad>, FA, FB, SCALE, true>(q, st);
-        return launch_tiles<MmWide, FA, FB, SCALE, true>(q, st);
+        return deep ? launch_tiles<MmDeep, FA, FB, SCALE, true>(q, st) : launch_tiles<MmWide, FA, FB, SCALE, true>(q, st);
       });
     });
   });

@@ -80,6 +80,20 @@ def test_matmul(out, e8m0, tile):
         check(product(a, b, out, n + (0, 4, 3)[i % 3]), a, b, out, (m, n, k))
 
 
+@pytest.mark.parametrize("scales", ((False, True), (False, False), (True, True)))
+@pytest.mark.parametrize("out", tuple(OUT))
+def test_matmul_large(out, scales):
+    """Sizes that take the 128 x 128 tiles, with two and with four stages, and the 256 x 256 ones; whole ones and some cut off."""
+    for i, (m, n, k) in enumerate([(1000, 2050, 400), (1024, 2048, 1100), (1000, 2050, 1601), (3900, 4100, 300)]):
+        a = coded(m, k, 0, scales[0], False, 3 * i, tight=i == 2)
+        b = coded(n, k, 0, scales[0], scales[1], 3 * i + 1)
+        check(product(a, b, out, n + (0, 4, 3)[i % 3]), a, b, out, (m, n, k))
+    for k in (512, 1100):
+        a, b = coded(129, k, 1, scales[0], False, 9), coded(260, k, 1, scales[0], scales[1], 10)
+        if out != torch.float16:  # whose range the products of E5M2 pass
+            check(product(a, b, out), a, b, out, ("e5m2", k))
+
+
 @pytest.mark.parametrize("formats", ((0, 1), (1, 0), (1, 1)))
 @pytest.mark.parametrize("out", (torch.float32, torch.bfloat16))
 def test_matmul_formats(out, formats):
