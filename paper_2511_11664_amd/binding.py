@@ -303,88 +303,94 @@ _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
-def _on(first, *more):
-    """The first tensor's device, None where a tensor is in host memory or on another device."""
-    dev = first.get_device()
-    if dev < 0:
+class _Refused(Exception):
+    pass
+
+
+def _mem(t, dev, rows, cols, ld, size):
+    """Address of a tensor on device `dev` whose memory reaches to the end of rows x cols elements of `size` bytes that are ld
+    apart; None for an absent one."""
+    if t is None:
         return None
-    for t in more:
-        if t is not None and t.get_device() != dev:
-            return None
-    return dev
-
-
-def _enqueue(entry, dev, *args):
-    """entry(*args, the current stream on `dev`).  Every device's default stream has the same handle, which stands for the
-    current device's: that is `dev` for the call."""
-    if _current_device() == dev:
-        return entry(*args, _raw_stream(dev))
-    with torch.cuda.device(dev):
-        return entry(*args, _raw_stream(dev))
-
-
-def _at(t):
-    return None if t is None else t.data_ptr()
-
-
-def _holds(t, rows, cols, ld, size):
-    """Whether a tensor's memory reaches to the end of rows x cols elements of `size` bytes that are ld apart; an absent one does."""
-    if t is None or not rows or not cols:
-        return True
-    return ((rows - 1) * ld + cols) * size <= _bytes(t)
-
-
-def _bytes(t):
-    """Bytes of memory from a tensor's first element on that it has for sure."""
-    return 0 if t is None else t.nbytes if t.is_contiguous() else _reach(t) * t.element_size()
+    if t.get_device() != dev or (rows and cols and ((rows - 1) * ld + cols) * size > (t.nbytes if t.is_contiguous() else _reach(t))):
+        raise _Refused
+    return t.data_ptr()
 
 
 def _reach(t):
-    """Elements from a tensor's first one to the last one that it can see."""
+    """Bytes from a tensor's first element to the last one that it can see."""
     n = 1
     for size, stride in zip(t.shape, t.stride()):
         if size == 0:
             return 0
         n += (size - 1) * stride
-    return n
+    return n * t.element_size()
 
 
-def _holds_blocks(code, scale, b):
-    rows, cols = b.rows, b.cols
-    if not rows or not cols:
-        return True
-    return _holds(code, rows, cols, b.ld, 1) and _holds(scale, (rows + BLOCK - 1) // BLOCK if b.block else rows, (cols + BLOCK - 1) // BLOCK, b.ld_scale,
-                                                        1 if b.scale_type else 4)
+def _mem_blocks(code, scale, dev, b):
+    """Addresses of a coded matrix's codes and scales."""
+    rows, cols, nb = b.rows, b.cols, (b.cols + BLOCK - 1) // BLOCK
+    return (_mem(code, dev, rows, cols, b.ld, 1),
+            _mem(scale, dev, (rows + BLOCK - 1) // BLOCK if b.block else rows, nb, b.ld_scale, 1 if b.scale_type else 4))
+
+
+def _mem_ws(ws, dev):
+    """Address and bytes of a workspace."""
+    if ws is None:
+        return None, 0
+    return _mem(ws, dev, 0, 0, 0, 0), ws.nbytes if ws.is_contiguous() else _reach(ws)
 
 
 def _size(dtype):
     return 2 if dtype else 4
 
 
-def rans_block_quantize(d_x, ld_x, in_dtype, transpose, d_code, d_scale, out) -> int:
-    dev = _on(d_x, d_code, d_scale)
-    if dev is None or not _holds_blocks(d_code, d_scale, out) or not _holds(d_x, *((out.cols, out.rows) if transpose else (out.rows, out.cols)), ld_x,
-                                                                                 _size(in_dtype)):
+def _enqueue(entry, dev, *args):
+    """entry(*args, the current stream on `dev`).  Every device's default stream has the same handle, which stands for the
+    current device's: that is `dev` for the call."""
+    if dev < 0:  # host memory
         return ERR_ARG
-    return _enqueue(lib().rans_block_quantize, dev, _at(d_x), ld_x, in_dtype, transpose, _at(d_code), _at(d_scale), out)
+    if _current_device() == dev:
+        return entry(*args, _raw_stream(dev))
+    with torch.cuda.device(dev):
+        return entry(*args, _raw_stream(dev))
+
+
+def rans_block_quantize(d_x, ld_x, in_dtype, transpose, d_code, d_scale, out) -> int:
+    dev = d_x.get_device()
+    try:
+        rows, cols = (out.cols, out.rows) if transpose else (out.rows, out.cols)
+        x = _mem(d_x, dev, rows, cols, ld_x, _size(in_dtype))
+        code, scale = _mem_blocks(d_code, d_scale, dev, out)
+    except _Refused:
+        return ERR_ARG
+    return _enqueue((_lib or lib()).rans_block_quantize, dev, x, ld_x, in_dtype, transpose, code, scale, out)
 
 
 def rans_block_dequantize(d_code, d_scale, blocks, out_dtype, d_x_out, ld_x) -> int:
-    dev = _on(d_x_out, d_code, d_scale)
-    if dev is None or not _holds_blocks(d_code, d_scale, blocks) or not _holds(d_x_out, blocks.rows, blocks.cols, ld_x, _size(out_dtype)):
+    dev = d_x_out.get_device()
+    try:
+        code, scale = _mem_blocks(d_code, d_scale, dev, blocks)
+        x = _mem(d_x_out, dev, blocks.rows, blocks.cols, ld_x, _size(out_dtype))
+    except _Refused:
         return ERR_ARG
-    return _enqueue(lib().rans_block_dequantize, dev, _at(d_code), _at(d_scale), blocks, out_dtype, _at(d_x_out), ld_x)
+    return _enqueue((_lib or lib()).rans_block_dequantize, dev, code, scale, blocks, out_dtype, x, ld_x)
 
 
 def rans_norm_quantize(d_x, d_res, d_weight, p, d_sum, d_rstd, d_y, d_code, d_scale, out) -> int:
-    dev = _on(d_x, d_res, d_weight, d_sum, d_rstd, d_y, d_code, d_scale)
-    rows, cols, e = p.rows, p.cols, _size(p.dtype)
-    if dev is None or not (_holds(d_x, rows, cols, p.ld_x, e) and _holds(d_res, rows, cols, p.ld_res, e) and _holds(d_sum, rows, cols, p.ld_sum, e)
-                          and _holds(d_y, rows, cols, p.ld_y, e) and _holds(d_weight, 1, cols, cols, _size(p.weight_dtype))
-                          and _holds(d_rstd, 1, rows, rows, 4)
-                          and (d_code is None or (out is not None and _holds_blocks(d_code, d_scale, out)))):
+    dev, rows, cols, e = d_x.get_device(), p.rows, p.cols, _size(p.dtype)
+    try:
+        x, res = _mem(d_x, dev, rows, cols, p.ld_x, e), _mem(d_res, dev, rows, cols, p.ld_res, e)
+        weight, rstd = _mem(d_weight, dev, 1, cols, cols, _size(p.weight_dtype)), _mem(d_rstd, dev, 1, rows, rows, 4)
+        total, y = _mem(d_sum, dev, rows, cols, p.ld_sum, e), _mem(d_y, dev, rows, cols, p.ld_y, e)
+        code = scale = None
+        if d_code is not None:
+            if out is None:
+                return ERR_ARG
+            code, scale = _mem_blocks(d_code, d_scale, dev, out)
+    except _Refused:
         return ERR_ARG
-    return _enqueue(lib().rans_norm_quantize, dev, _at(d_x), _at(d_res), _at(d_weight), p, _at(d_sum), _at(d_rstd), _at(d_y), _at(d_code), _at(d_scale), out)
+    return _enqueue((_lib or lib()).rans_norm_quantize, dev, x, res, weight, p, total, rstd, y, code, scale, out)
 
 
 def rans_norm_workspace_bytes(p: NormParams):
@@ -394,14 +400,16 @@ def rans_norm_workspace_bytes(p: NormParams):
 
 
 def rans_norm_backward(d_dy, d_dsum, d_sum, d_weight, d_rstd, p, d_dx, d_dweight, d_ws) -> int:
-    dev = _on(d_dy, d_dsum, d_sum, d_weight, d_rstd, d_dx, d_dweight, d_ws)
-    rows, cols, e = p.rows, p.cols, _size(p.dtype)
-    if dev is None or not (_holds(d_dy, rows, cols, p.ld_y, e) and _holds(d_dsum, rows, cols, p.ld_res, e) and _holds(d_sum, rows, cols, p.ld_sum, e)
-                          and _holds(d_dx, rows, cols, p.ld_x, e) and _holds(d_weight, 1, cols, cols, _size(p.weight_dtype))
-                          and _holds(d_rstd, 1, rows, rows, 4) and _holds(d_dweight, 1, cols, cols, 4)):
+    dev, rows, cols, e = d_dy.get_device(), p.rows, p.cols, _size(p.dtype)
+    try:
+        dy, dsum = _mem(d_dy, dev, rows, cols, p.ld_y, e), _mem(d_dsum, dev, rows, cols, p.ld_res, e)
+        total, dx = _mem(d_sum, dev, rows, cols, p.ld_sum, e), _mem(d_dx, dev, rows, cols, p.ld_x, e)
+        weight, rstd = _mem(d_weight, dev, 1, cols, cols, _size(p.weight_dtype)), _mem(d_rstd, dev, 1, rows, rows, 4)
+        dweight = _mem(d_dweight, dev, 1, cols, cols, 4)
+        ws, ws_bytes = _mem_ws(d_ws, dev)
+    except _Refused:
         return ERR_ARG
-    return _enqueue(lib().rans_norm_backward, dev, _at(d_dy), _at(d_dsum), _at(d_sum), _at(d_weight), _at(d_rstd), p, _at(d_dx), _at(d_dweight), _at(d_ws),
-                    _bytes(d_ws))
+    return _enqueue((_lib or lib()).rans_norm_backward, dev, dy, dsum, total, weight, rstd, p, dx, dweight, ws, ws_bytes)
 
 
 def rans_matmul_workspace_bytes(a: Blocks, b: Blocks):
@@ -411,11 +419,15 @@ def rans_matmul_workspace_bytes(a: Blocks, b: Blocks):
 
 
 def rans_block_matmul(d_a, d_a_scale, a, d_b, d_b_scale, b, out_dtype, d_c, ld_c, d_ws) -> int:
-    dev = _on(d_c, d_a, d_a_scale, d_b, d_b_scale, d_ws)
-    if dev is None or not (_holds_blocks(d_a, d_a_scale, a) and _holds_blocks(d_b, d_b_scale, b) and _holds(d_c, a.rows, b.rows, ld_c, _size(out_dtype))):
+    dev = d_c.get_device()
+    try:
+        code_a, scale_a = _mem_blocks(d_a, d_a_scale, dev, a)
+        code_b, scale_b = _mem_blocks(d_b, d_b_scale, dev, b)
+        c = _mem(d_c, dev, a.rows, b.rows, ld_c, _size(out_dtype))
+        ws, ws_bytes = _mem_ws(d_ws, dev)
+    except _Refused:
         return ERR_ARG
-    return _enqueue(lib().rans_block_matmul, dev, _at(d_a), _at(d_a_scale), a, _at(d_b), _at(d_b_scale), b, out_dtype, _at(d_c), ld_c, _at(d_ws),
-                    _bytes(d_ws))
+    return _enqueue((_lib or lib()).rans_block_matmul, dev, code_a, scale_a, a, code_b, scale_b, b, out_dtype, c, ld_c, ws, ws_bytes)
 
 
 class BlockMatrix:

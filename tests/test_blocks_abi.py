@@ -149,10 +149,23 @@ def test_binding_refuses_host_tensors_and_short_memory(lib):
     assert B.rans_norm_quantize(x, None, None, norm_params(dtype=B.F32, weight_dtype=B.F32), None, None, x, None, None, None) == B.ERR_ARG
     assert B.rans_norm_backward(x, None, x, None, x[0], norm_params(dtype=B.F32, weight_dtype=B.F32), x, None, None) == B.ERR_ARG
     assert B.rans_block_matmul(code, scale, b, code, scale, b, B.F32, x, 256, None) == B.ERR_ARG
-    assert B._holds(x, 4, 256, 256, 4) and not B._holds(x, 4, 256, 257, 4) and not B._holds(x, 5, 1, 256, 4) and B._holds(x[:, :7], 4, 7, 256, 4)
-    assert not B._holds(x.half(), 4, 256, 256, 4)                       # elements of half the size
-    assert not B._holds(x[0].expand(8, 256), 8, 256, 256, 4)            # one row of memory, seen eight times
-    assert not B._holds_blocks(code, scale, blocks(rows=5)) and B._holds_blocks(code, scale[:1], blocks(block=1))
+    host = -1
+
+    def holds(t, *want):
+        try:
+            return B._mem(t, host, *want) == t.data_ptr()
+        except B._Refused:
+            return False
+
+    assert holds(x, 4, 256, 256, 4) and not holds(x, 4, 256, 257, 4) and not holds(x, 5, 1, 256, 4) and holds(x[:, :7], 4, 7, 256, 4)
+    assert not holds(x.half(), 4, 256, 256, 4)                       # elements of half the size
+    assert not holds(x[0].expand(8, 256), 8, 256, 256, 4)            # one row of memory, seen eight times
+    assert B._mem(None, host, 4, 256, 256, 4) is None
+    with pytest.raises(B._Refused):
+        B._mem(x, 0, 4, 256, 256, 4)                                 # on another device
+    with pytest.raises(B._Refused):
+        B._mem_blocks(code, scale, host, blocks(rows=5))
+    assert B._mem_blocks(code, scale[:1], host, blocks(block=1)) == (code.data_ptr(), scale.data_ptr())
     with pytest.raises(B.RansError):
         B._ld(x.t())
 
@@ -200,5 +213,8 @@ def test_calls_go_to_their_tensors_device(monkeypatch):
 
 def test_memory_of_a_workspace():
     whole = torch.empty(4, 256, dtype=torch.float32)
-    assert B._bytes(None) == 0 and B._bytes(whole) == 4096 and B._bytes(whole[1:]) == 3072
-    assert B._bytes(torch.empty(1, dtype=torch.uint8).expand(4096)) == 1 and B._bytes(whole[:, :128]) == (3 * 256 + 128) * 4
+    at = whole.data_ptr()
+    assert B._mem_ws(None, -1) == (None, 0) and B._mem_ws(whole, -1) == (at, 4096) and B._mem_ws(whole[1:], -1) == (at + 1024, 3072)
+    assert B._mem_ws(torch.empty(1, dtype=torch.uint8).expand(4096), -1)[1] == 1 and B._mem_ws(whole[:, :128], -1) == (at, (3 * 256 + 128) * 4)
+    with pytest.raises(B._Refused):
+        B._mem_ws(whole, 0)
