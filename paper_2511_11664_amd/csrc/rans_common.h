@@ -1,6 +1,7 @@
 // rans_common.h -- constants, workspace layout, device helpers shared by all kernels
 //
-// Part of the one translation unit rans_if.hip (included there, in this order); not a stand-alone header.
+// Part of the translation unit rans_if.hip (included there, in this order) and, for its constants and helpers, of the other
+// ones; not a stand-alone header.
 #pragma once
 
 namespace {
