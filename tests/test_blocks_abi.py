@@ -212,9 +212,9 @@ def test_calls_go_to_their_tensors_device(monkeypatch):
 
 
 def test_memory_of_a_workspace():
-    whole = torch.empty(4, 256, dtype=torch.float32)
+    whole = torch.empty(5, 256, dtype=torch.float32)
     at = whole.data_ptr()
-    assert B._mem_ws(None, -1) == (None, 0) and B._mem_ws(whole, -1) == (at, 4096) and B._mem_ws(whole[1:], -1) == (at + 1024, 3072)
-    assert B._mem_ws(torch.empty(1, dtype=torch.uint8).expand(4096), -1)[1] == 1 and B._mem_ws(whole[:, :128], -1) == (at, (3 * 256 + 128) * 4)
+    assert B._mem_ws(None, -1) == (None, 0) and B._mem_ws(whole, -1) == (at, 5120) and B._mem_ws(whole[1:], -1) == (at + 1024, 4096)
+    assert B._mem_ws(torch.empty(1, dtype=torch.uint8).expand(4096), -1)[1] == 1 and B._mem_ws(whole[:, :128], -1) == (at, (4 * 256 + 128) * 4)
     with pytest.raises(B._Refused):
         B._mem_ws(whole, 0)
