@@ -257,7 +257,8 @@ int rans_norm_quantize(const void *d_x, const void *d_res, const void *d_weight,
  * to h from elsewhere (rows ld_res apart; NULL: none), d_sum: h (rows ld_sum apart), d_rstd: as the forward call left it.
  *   d_dx (rows ld_x apart) = rstd * (dy w - xh * mean(dy w xh)) + dsum, xh = h * rstd: the gradient of x and of the residual;
  *   d_dweight (cols binary32 numbers; NULL: not wanted) = sum over the rows of dy * xh, always added in the same order.
- * d_dx may be d_dy's, d_dsum's or d_sum's own memory.  Workspace (only where d_dweight is given): rans_norm_workspace_bytes(). */
+ * d_dx may be d_dy's, d_dsum's or d_sum's own memory (same pointer, same ld; the bits of d_dweight may
+ * differ from those of a call with memory of its own).  Workspace (only where d_dweight is given): rans_norm_workspace_bytes(). */
 int rans_norm_workspace_bytes(const rans_norm_params *p, size_t *ws_bytes);
 int rans_norm_backward(const void *d_dy, const void *d_dsum, const void *d_sum, const void *d_weight, const float *d_rstd,
                        const rans_norm_params *p, void *d_dx, float *d_dweight, void *d_ws, size_t ws_bytes, void *stream);

@@ -214,6 +214,17 @@ uint32_t norm_parts(const rans_norm_params &p) {
   return (uint32_t)((p.rows + each - 1) / each);
 }
 
+// Both gradients from one kernel, dy and h read twice, or partial rows and a second kernel to add them up: one for as many rows as
+// stay in the caches and keep the columns' work-groups short.  One / two kernels, us: 8 x 4096 3.2 / 5.5, 395 x 1024 5.5 / 7.1, 395 x
+// 5120 5.9 / 9.2, 1024 x 4096 9.8 / 11.7; 2048 x 4096 28.3 / 16.8, 1024 x 512 24.8 / 8.0.
+bool norm_both(const rans_norm_params &p, uint32_t threads) { return p.rows <= 2 * threads && p.rows * p.cols <= 1u << 22; }
+
+// Whether two matrices of the same shape have memory in common.
+bool overlap(const void *a, uint64_t ld_a, const void *b, uint64_t ld_b, uint64_t rows, uint64_t cols, size_t eb) {
+  const uintptr_t pa = (uintptr_t)a, pb = (uintptr_t)b;
+  return pa < pb + ((rows - 1) * ld_b + cols) * eb && pb < pa + ((rows - 1) * ld_a + cols) * eb;
+}
+
 }  // namespace
 
 extern "C" {
@@ -299,6 +310,8 @@ int rans_norm_backward(const void *d_dy, const void *d_dsum, const void *d_sum, 
   a.ld_dy = p->ld_y, a.ld_dsum = p->ld_res, a.ld_h = p->ld_sum, a.ld_dx = p->ld_x;
   a.rows = p->rows, a.cols = (uint32_t)p->cols, a.inv_cols = 1.0f / (float)p->cols;
   const uint32_t g = norm_parts(*p);
+  bool both = d_dweight && p->rows && !overlap(d_dx, p->ld_x, d_dy, p->ld_y, p->rows, p->cols, eb) &&
+              !overlap(d_dx, p->ld_x, d_sum, p->ld_sum, p->rows, p->cols, eb);
   if (g) {
     rc = by_dtype(p->dtype, [&](auto elem) {
       typedef decltype(elem) T;
@@ -306,7 +319,14 @@ int rans_norm_backward(const void *d_dy, const void *d_dsum, const void *d_sum, 
         typedef typename std::conditional<decltype(same_tag)::value, T, float>::type W;
         return by_row_backward(*p, [&](auto nt_tag, auto nv_tag) -> int {
           constexpr int NT = decltype(nt_tag)::value, NV = decltype(nv_tag)::value;
-          PROF_LAUNCH(KID_NORM_BWD, (k_norm_bwd<T, W, NT, NV>), dim3(g), dim3(NT), 0, st, a);
+          both = both && norm_both(*p, NT);
+          if (both) {
+            const uint32_t n_dw = (uint32_t)((p->cols + 63) / 64);
+            a.part = nullptr;
+            PROF_LAUNCH(KID_NORM_BWD_BOTH, (k_norm_bwd_both<T, W, NT, NV>), dim3(n_dw + (uint32_t)p->rows), dim3(NT), 0, st, a, d_dweight, n_dw);
+          } else {
+            PROF_LAUNCH(KID_NORM_BWD, (k_norm_bwd<T, W, NT, NV>), dim3(g), dim3(NT), 0, st, a);
+          }
           LAUNCH_CHECK();
           return RANS_OK;
         });
@@ -314,7 +334,7 @@ int rans_norm_backward(const void *d_dy, const void *d_dsum, const void *d_sum, 
     });
     if (rc) return rc;
   }
-  if (d_dweight) {
+  if (d_dweight && !both) {
     PROF_LAUNCH(KID_NORM_DW, k_norm_dw, dim3((uint32_t)((p->cols + 31) / 32)), dim3(kDwWG), 0, st, (const float *)d_ws, g, (uint32_t)p->cols,
                 d_dweight);
     LAUNCH_CHECK();

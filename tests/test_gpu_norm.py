@@ -237,3 +237,31 @@ def test_norm_offsets_beyond_32_bits():
     h, _, y = O.norm(x, r, w.to(torch.bfloat16), EPS, torch.bfloat16)
     assert torch.equal(xd.cpu().double(), h)
     assert ((out.cpu().double() - y).abs() <= (rstd_tolerance(cols) + 3 * U) * 1.01 * y.abs() + half_step(y, torch.bfloat16)).all()
+
+
+@pytest.mark.parametrize("over", ("dy", "dsum", "h", "none"))
+def test_norm_backward_weight_gradient_with_dx_in_place(over, launched_kernels):
+    """dx in the memory that the weight's gradient is read from: two kernels, one after the other; elsewhere one for both."""
+    for rows, cols in ((5, 300), (40, 1000), (395, 4096), (100, 8200)):
+        dy, ds, h, w, rstd = bwd_data(rows, cols, torch.bfloat16, False)
+        t = dict(dy=dy.cuda(), dsum=ds.cuda(), h=h.cuda(), none=torch.empty_like(h, device="cuda"))
+        p = params(rows, cols, torch.bfloat16, w.dtype)
+        dw, ws = torch.empty(cols, device="cuda"), B.workspace(B.rans_norm_workspace_bytes(p)[1])
+        args = (t["dy"], t["dsum"], t["h"], w.cuda(), rstd.cuda(), p, t[over], dw, ws)
+
+        def call():
+            assert B.rans_norm_backward(*args) == 0
+
+        names = launched_kernels(call)
+        check_backward(rows, cols, torch.bfloat16, dy, ds, h, w, rstd, t[over], dw)
+        assert names == ({"k_norm_bwd", "k_norm_dw"} if over in ("dy", "h") else {"k_norm_bwd_both"})
+
+
+def test_norm_backward_kernels_by_rows(launched_kernels):
+    for (rows, cols), names in {(1, 512): {"k_norm_bwd_both"}, (1000, 512): {"k_norm_bwd", "k_norm_dw"}, (300, 2048): {"k_norm_bwd_both"}, (1100, 4096): {"k_norm_bwd", "k_norm_dw"}}.items():
+        dy, ds, h, w, rstd = bwd_data(rows, cols, torch.float16, True)
+        p = params(rows, cols, torch.float16, w.dtype)
+        dx, dw, ws = torch.empty_like(h, device="cuda"), torch.empty(cols, device="cuda"), B.workspace(B.rans_norm_workspace_bytes(p)[1])
+        args = [t.cuda() for t in (dy, ds, h, w, rstd)]
+        assert launched_kernels(lambda: B.rans_norm_backward(*args, p, dx, dw, ws)) == names
+        check_backward(rows, cols, torch.float16, dy, ds, h, w, rstd, dx, dw)
