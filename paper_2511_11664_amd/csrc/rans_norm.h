@@ -3,7 +3,8 @@
 // Part of the translation unit rans_blocks.hip; not a stand-alone header.
 //
 // Forward, a row of K elements:  h = x + residual, rounded to the stream's type, because that is what the next residual
-// addition and the backward pass read;  rstd = 1 / sqrt(sum h^2 / K + eps);  y = h * rstd * w in binary32;  codes and scales
+// addition and the backward pass read;  rstd = 1 / sqrt(sum h^2 / K + eps);  y = h * rstd * w, half a step of binary32 off
+// and a little (rstd is kept in two parts);  codes and scales
 // of y by the row blocks of rans_blocks.h, and / or y itself rounded once.
 // Backward:  g = dy * w, xh = h * rstd;  dx = rstd * (g - xh * sum(g * xh) / K) + dsum;  dw = sum over rows of dy * xh.
 // All sums are binary32: a lane's own eight neighbours (and every further eight), then the lanes of a wave, then the waves.
@@ -38,8 +39,24 @@ struct NormFwd {
   void *scales;
   uint64_t ld_x, ld_res, ld_sum, ld_y, ld, ld_scale;
   uint32_t cols, e5m2;
-  float eps, inv_cols;
+  float eps, inv_cols, inv_cols_low;  // 1 / cols in two parts
 };
+
+// 1 / sqrt(sum / cols + eps) to about 2^-46, as the nearest binary32 number and what it leaves.  The approximate reciprocal root
+// r of the mean m, whose own rounding errors are kept beside it, has one step r + r / 2 (1 - m r^2).  Codes are a rounding of y
+// to a few bits: with y off by half a step of binary32 and not by one or two, half as many of them fall on the wrong side.
+struct Rstd {
+  float r, low;
+};
+__device__ __forceinline__ Rstd rstd_of(float sum, const NormFwd &a) {
+  const float q = sum * a.inv_cols, q_low = __builtin_fmaf(sum, a.inv_cols_low, __builtin_fmaf(sum, a.inv_cols, -q));
+  const float m = q + a.eps, part = m - q, m_low = ((q - (m - part)) + (a.eps - part)) + q_low;
+  if (!(m >= 0x1p-100f && m < 0x1p100f)) return Rstd{1.0f / sqrtf(m), 0.0f};
+  const float r = __builtin_amdgcn_rsqf(m), t = m * r, t_low = __builtin_fmaf(m_low, r, __builtin_fmaf(m, r, -t));
+  const float step = 0.5f * r * __builtin_fmaf(-t_low, r, __builtin_fmaf(-t, r, 1.0f));
+  const float high = r + step;
+  return Rstd{high, (r - high) + step};
+}
 
 // A row per work-group of NT threads, NV times eight neighbouring elements a thread (NV = 0: any length, h read again).
 // Everything a thread needs from memory is requested before the row's sum, the weight too.  16384 x 4096 fp16 with a residual,
@@ -53,7 +70,8 @@ __global__ __launch_bounds__(NT) void k_norm_quant(NormFwd a, uint64_t row0) {
   const T *x = (const T *)a.x + row * a.ld_x;
   const T *res = a.res ? (const T *)a.res + row * a.ld_res : nullptr;
   T *sum = a.sum ? (T *)a.sum + row * a.ld_sum : nullptr;
-  float acc = 0, rstd = 0;
+  float acc = 0;
+  Rstd rstd = {0, 0};
   auto add = [&](V v, V r) {
     f32x8 h = float8_of(v);
     if (res) {
@@ -70,7 +88,11 @@ __global__ __launch_bounds__(NT) void k_norm_quant(NormFwd a, uint64_t row0) {
   auto give = [&](uint32_t c, f32x8 v, f32x8 w) {
     // 16 lanes hold a block; lanes behind the row's end hold zeros and take part in its maximum
 #pragma unroll
-    for (int i = 0; i < 8; i++) v[i] = v[i] * rstd * w[i];
+    for (int i = 0; i < 8; i++) {
+      // h * rstd in two parts times w; an infinite w meets the lower part as a finite one
+      const float x = v[i] * rstd.r, low = __builtin_fmaf(v[i], rstd.low, __builtin_fmaf(v[i], rstd.r, -x));
+      v[i] = __builtin_fmaf(x, w[i], low * __builtin_amdgcn_fmed3f(w[i], -0x1.fffffep127f, 0x1.fffffep127f));
+    }
     if (a.y && c < n) store8((T *)a.y + row * a.ld_y, c, n, v);
     if (a.codes) {
       const BlockScale s = block_scale<E8M0>(max16(abs_max8(v)), a.e5m2);
@@ -100,7 +122,7 @@ __global__ __launch_bounds__(NT) void k_norm_quant(NormFwd a, uint64_t row0) {
       if (sum && c < n) store8(sum, c, n, h[k]);
       square(h[k]);
     }
-    rstd = 1.0f / sqrtf(group_sum<NT>(acc, s_sum) * a.inv_cols + a.eps);
+    rstd = rstd_of(group_sum<NT>(acc, s_sum), a);
 #pragma unroll
     for (int k = 0; k < NV; k++) {
       const uint32_t c = (k * NT + t) * 8;
@@ -116,14 +138,14 @@ __global__ __launch_bounds__(NT) void k_norm_quant(NormFwd a, uint64_t row0) {
       if (sum) store8(sum, c, n, h);
       square(h);
     }
-    rstd = 1.0f / sqrtf(group_sum<NT>(acc, s_sum) * a.inv_cols + a.eps);
+    rstd = rstd_of(group_sum<NT>(acc, s_sum), a);
     for (uint32_t c = t * 8; (c & ~(kBlk - 1)) < n; c += NT * 8) {
       f32x8 h = {0, 0, 0, 0, 0, 0, 0, 0};
       if (c < n) h = sum ? load8((const T *)sum, c, n) : take(c);
       give(c, h, weight8(c));
     }
   }
-  if (a.rstd && t == 0) a.rstd[row] = rstd;
+  if (a.rstd && t == 0) a.rstd[row] = rstd.r;
 }
 
 struct NormBwd {

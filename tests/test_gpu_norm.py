@@ -265,3 +265,43 @@ def test_norm_backward_kernels_by_rows(launched_kernels):
         args = [t.cuda() for t in (dy, ds, h, w, rstd)]
         assert launched_kernels(lambda: B.rans_norm_backward(*args, p, dx, dw, ws)) == names
         check_backward(rows, cols, torch.float16, dy, ds, h, w, rstd, dx, dw)
+
+
+def test_norm_of_large_and_small_rows_and_infinite_weights():
+    """Means far from one; an infinite weight gives infinities of h's sign, NaN where h is zero."""
+    x, _, w = data(3, 1000, torch.float32)
+    w[5], w[6] = float("inf"), float("-inf")
+    x[0, 6] = 0
+    for size in (1e17, 1.0, 1e-16):
+        h = x * size
+        p = B.make_norm_params(3, 1000, B.F32, B.F32, 0.0)
+        out = torch.empty(3, 1000, device="cuda")
+        assert B.rans_norm_quantize(h.cuda(), None, w.cuda(), p, None, None, out, None, None, None) == 0
+        want = O.norm(h, None, w, 0.0, torch.float32)[2]
+        got = out.cpu().double()
+        assert got[0, 6].isnan() and got[1].isnan().all()  # 0 * inf; the row of zeros without eps
+        for row in (0, 2):
+            assert got[row, 5] == want[row, 5] and got[row, 5].isinf()
+        assert got[2, 6] == want[2, 6] and got[2, 6].isinf()
+        rest = torch.ones(1000, dtype=torch.bool)
+        rest[5:7] = False
+        for row in (0, 2):
+            assert ((got - want).abs()[row, rest] <= ((rstd_tolerance(1000) + 4 * U) * want.abs())[row, rest]).all(), size
+
+
+def test_norm_codes_are_the_definitions():
+    """y is half a step of binary32 off and a little, so that of codes under powers of two hardly one is not its definition's."""
+    rows, cols = 512, 4096
+    x, _, w = data(rows, cols, torch.bfloat16)
+    w = w.to(torch.bfloat16)
+    m = B.BlockMatrix(rows, cols, B.E4M3, B.SCALE_E8M0)
+    assert B.rans_norm_quantize(x.cuda(), None, w.cuda(), params(rows, cols, torch.bfloat16, w.dtype), None, None, None, m.code, m.scale, m.layout) == 0
+    y = O.norm(x, None, w, EPS, torch.bfloat16)[2]
+    s = O.spread(torch.exp2(m.scale[:, :cols // 128].cpu().double() - 127), rows, cols, False)
+    v = y / s
+    got = O.decode8(m.code[:, :cols].cpu(), 0)
+    step = torch.exp2(torch.clamp(torch.floor(torch.log2(got.abs().clamp(min=2.0 ** -9))), min=-6) - 3)
+    off = (got - v).abs() > step / 2 * (1 + 1e-9)
+    # a code is wrong where a multiple of half a step lies within y's error, some 2^-23 of y: of 2^21 codes about 2^21 2^-23 2^4 2 = 8
+    assert off.sum() <= 40
+    assert ((got - v).abs() <= step / 2 + 2.0 ** -22 * v.abs()).all()
