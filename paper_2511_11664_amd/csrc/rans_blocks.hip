@@ -251,8 +251,7 @@ int rans_norm_quantize(const void *d_x, const void *d_res, const void *d_weight,
   NormFwd a{};
   a.x = d_x, a.res = d_res, a.weight = d_weight, a.sum = d_sum, a.y = d_y, a.rstd = d_rstd, a.codes = d_code, a.scales = d_scale;
   a.ld_x = p->ld_x, a.ld_res = p->ld_res, a.ld_sum = p->ld_sum, a.ld_y = p->ld_y;
-  a.cols = (uint32_t)p->cols, a.eps = p->eps;
-  a.inv_cols = (float)(1.0 / (double)p->cols), a.inv_cols_low = (float)(1.0 / (double)p->cols - (double)a.inv_cols);
+  a.cols = (uint32_t)p->cols, a.eps = p->eps, a.inv_cols = 1.0 / (double)p->cols;
   if (d_code) {
     a.ld = out->ld, a.ld_scale = out->ld_scale, a.e5m2 = out->format;
   }

@@ -7,25 +7,23 @@
 // and a little (rstd is kept in two parts);  codes and scales
 // of y by the row blocks of rans_blocks.h, and / or y itself rounded once.
 // Backward:  g = dy * w, xh = h * rstd;  dx = rstd * (g - xh * sum(g * xh) / K) + dsum;  dw = sum over rows of dy * xh.
-// All sums are binary32: a lane's own eight neighbours (and every further eight), then the lanes of a wave, then the waves.
+// Sums of a row's squares: eight neighbours in binary32, whose errors average out, the rest in binary64, which costs two
+// instructions for eight elements.  The backward's sums are binary32: a lane's own eight neighbours (and every further eight),
+// then the lanes of a wave, then the waves.
 //
 // Bound by memory: each tensor is read once and written once, a row lives in registers between its sum and its output.
 #pragma once
 
 namespace {
 
-// Sum over a work-group of NT threads, in every thread.  `s`: NT / 64 floats per value; two values at most.
-template <int NT> __device__ inline float wave_sum(float v) {
+// Sum over a work-group of NT threads, in every thread.  `s`: NT / 64 numbers.
+template <int NT, typename N> __device__ inline N group_sum(N v, N *s) {
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-  return v;
-}
-template <int NT> __device__ inline float group_sum(float v, float *s) {
-  v = wave_sum<NT>(v);
   if (NT == 64) return v;
   if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
   __syncthreads();
-  float r = 0;
+  N r = 0;
 #pragma unroll
   for (int w = 0; w < NT / 64; w++) r += s[w];
   return r;
@@ -39,7 +37,8 @@ struct NormFwd {
   void *scales;
   uint64_t ld_x, ld_res, ld_sum, ld_y, ld, ld_scale;
   uint32_t cols, e5m2;
-  float eps, inv_cols, inv_cols_low;  // 1 / cols in two parts
+  float eps;
+  double inv_cols;
 };
 
 // 1 / sqrt(sum / cols + eps) to about 2^-46, as the nearest binary32 number and what it leaves.  The approximate reciprocal root
@@ -48,9 +47,9 @@ struct NormFwd {
 struct Rstd {
   float r, low;
 };
-__device__ __forceinline__ Rstd rstd_of(float sum, const NormFwd &a) {
-  const float q = sum * a.inv_cols, q_low = __builtin_fmaf(sum, a.inv_cols_low, __builtin_fmaf(sum, a.inv_cols, -q));
-  const float m = q + a.eps, part = m - q, m_low = ((q - (m - part)) + (a.eps - part)) + q_low;
+__device__ __forceinline__ Rstd rstd_of(double sum, const NormFwd &a) {
+  const double mean = sum * a.inv_cols + (double)a.eps;
+  const float m = (float)mean, m_low = (float)(mean - (double)m);
   if (!(m >= 0x1p-100f && m < 0x1p100f)) return Rstd{1.0f / sqrtf(m), 0.0f};
   const float r = __builtin_amdgcn_rsqf(m), t = m * r, t_low = __builtin_fmaf(m_low, r, __builtin_fmaf(m, r, -t));
   const float step = 0.5f * r * __builtin_fmaf(-t_low, r, __builtin_fmaf(-t, r, 1.0f));
@@ -64,13 +63,13 @@ __device__ __forceinline__ Rstd rstd_of(float sum, const NormFwd &a) {
 template <typename T, typename W, bool E8M0, int NT, int NV>
 __global__ __launch_bounds__(NT) void k_norm_quant(NormFwd a, uint64_t row0) {
   typedef typename Vec8<T>::type V;
-  __shared__ float s_sum[NT / 64];
+  __shared__ double s_sum[NT / 64];
   const uint64_t row = row0 + blockIdx.x;
   const uint32_t t = threadIdx.x, n = a.cols;
   const T *x = (const T *)a.x + row * a.ld_x;
   const T *res = a.res ? (const T *)a.res + row * a.ld_res : nullptr;
   T *sum = a.sum ? (T *)a.sum + row * a.ld_sum : nullptr;
-  float acc = 0;
+  double acc = 0;
   Rstd rstd = {0, 0};
   auto add = [&](V v, V r) {
     f32x8 h = float8_of(v);
@@ -81,8 +80,10 @@ __global__ __launch_bounds__(NT) void k_norm_quant(NormFwd a, uint64_t row0) {
     return h;
   };
   auto square = [&](f32x8 h) {
+    float q[4];
 #pragma unroll
-    for (int i = 0; i < 8; i++) acc = __builtin_fmaf(h[i], h[i], acc);
+    for (int i = 0; i < 4; i++) q[i] = __builtin_fmaf(h[i], h[i], h[i + 4] * h[i + 4]);
+    acc += (double)((q[0] + q[1]) + (q[2] + q[3]));
   };
   auto weight8 = [&](uint32_t c) { return a.weight ? load8((const W *)a.weight, c, n) : (f32x8){1, 1, 1, 1, 1, 1, 1, 1}; };
   auto give = [&](uint32_t c, f32x8 v, f32x8 w) {
