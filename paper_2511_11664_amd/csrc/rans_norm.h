@@ -4,8 +4,7 @@
 //
 // Forward, a row of K elements:  h = x + residual, rounded to the stream's type, because that is what the next residual
 // addition and the backward pass read;  rstd = 1 / sqrt(sum h^2 / K + eps);  y = h * rstd * w, half a step of binary32 off
-// and a little (rstd is kept in two parts);  codes and scales
-// of y by the row blocks of rans_blocks.h, and / or y itself rounded once.
+// and a little (rstd is kept in two parts);  codes and scales of y by the row blocks of rans_blocks.h, and / or y itself.
 // Backward:  g = dy * w, xh = h * rstd;  dx = rstd * (g - xh * sum(g * xh) / K) + dsum;  dw = sum over rows of dy * xh.
 // Sums of a row's squares: eight neighbours in binary32, whose errors average out, the rest in binary64, which costs two
 // instructions for eight elements.  The backward's sums are binary32: a lane's own eight neighbours (and every further eight),
@@ -41,9 +40,9 @@ struct NormFwd {
   double inv_cols;
 };
 
-// 1 / sqrt(sum / cols + eps) to about 2^-46, as the nearest binary32 number and what it leaves.  The approximate reciprocal root
-// r of the mean m, whose own rounding errors are kept beside it, has one step r + r / 2 (1 - m r^2).  Codes are a rounding of y
-// to a few bits: with y off by half a step of binary32 and not by one or two, half as many of them fall on the wrong side.
+// 1 / sqrt(sum / cols + eps) as the nearest binary32 number and what it leaves: the approximate reciprocal root r of the mean m,
+// whose own rounding errors are kept beside it, takes one step r + r / 2 (1 - m r^2).  Codes are a rounding of y to a few bits,
+// and y is off by half a step of binary32 and not by one or two, so that fewer of them fall on the other side of a tie.
 struct Rstd {
   float r, low;
 };
