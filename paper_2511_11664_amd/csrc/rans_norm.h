@@ -85,17 +85,33 @@ __global__ __launch_bounds__(NT) void k_norm_quant(NormFwd a, uint64_t row0) {
     acc += (double)((q[0] + q[1]) + (q[2] + q[3]));
   };
   auto weight8 = [&](uint32_t c) { return a.weight ? load8((const W *)a.weight, c, n) : (f32x8){1, 1, 1, 1, 1, 1, 1, 1}; };
-  auto give = [&](uint32_t c, f32x8 v, f32x8 w) {
+  auto give = [&](uint32_t c, f32x8 h8, f32x8 w) {
     // 16 lanes hold a block; lanes behind the row's end hold zeros and take part in its maximum
+    // h * rstd in two parts times w; an infinite w meets the lower part as a finite one
+    auto lower = [&](int i, float x) { return __builtin_fmaf(h8[i], rstd.low, __builtin_fmaf(h8[i], rstd.r, -x)) * __builtin_amdgcn_fmed3f(w[i], -0x1.fffffep127f, 0x1.fffffep127f); };
+    f32x8 v;
+    uint32_t tie = 1;  // 0 where a y lies halfway between two codes, as far as its binary32 tells
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-      // h * rstd in two parts times w; an infinite w meets the lower part as a finite one
-      const float x = v[i] * rstd.r, low = __builtin_fmaf(v[i], rstd.low, __builtin_fmaf(v[i], rstd.r, -x));
-      v[i] = __builtin_fmaf(x, w[i], low * __builtin_amdgcn_fmed3f(w[i], -0x1.fffffep127f, 0x1.fffffep127f));
+      const float x = h8[i] * rstd.r;
+      v[i] = __builtin_fmaf(x, w[i], lower(i, x));
+      if (E8M0) {
+        const uint32_t t = (__float_as_uint(v[i]) << (a.e5m2 ? 11 : 12)) + 0x80000000u;
+        tie = t < tie ? t : tie;
+      }
     }
     if (a.y && c < n) store8((T *)a.y + row * a.ld_y, c, n, v);
     if (a.codes) {
       const BlockScale s = block_scale<E8M0>(max16(abs_max8(v)), a.e5m2);
+      if (E8M0 && tie == 0) {
+        // powers of two leave a y where it is between two codes: what binary32 dropped decides
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+          const uint32_t b = __float_as_uint(v[i]);
+          const float x = h8[i] * rstd.r, rest = __builtin_fmaf(x, w[i], -v[i]) + lower(i, x);
+          if ((b << (a.e5m2 ? 11 : 12)) == 0x80000000u && rest != 0) v[i] = __uint_as_float((rest > 0) == (v[i] > 0) ? b + 1 : b - 1);
+        }
+      }
       if (c < n) {
         store_codes8(a.codes + row * a.ld, c, n, codes8(v, s.factor, a.e5m2));
         if ((t & 15) == 0) store_scale<E8M0>(a.scales, row * a.ld_scale + c / kBlk, s);
