@@ -358,12 +358,23 @@ int check_matmul(const rans_blocks *a, const rans_blocks *b) {
   return RANS_OK;
 }
 
-size_t matmul_ws_bytes(const rans_blocks *a, const rans_blocks *b) {
-  const MatmulParts parts = matmul_parts(a->rows, b->rows, a->cols);
-  return parts.n < 2 ? 0 : align_up((size_t)parts.n * a->rows * matmul_part_ld(b->rows) * 4, 256);
-}
-
 constexpr uint64_t kMatmulSlice = 1u << 17;  // rows of A and of B in a launch: 2^22 of the smallest tiles; whole tiles of scales
+
+// Enough for each of the launches, which follow one another: whether K goes in parts is decided for a launch's own rows, and
+// the last rows of a long matrix may have few enough tiles where the ones before had not.
+size_t matmul_ws_bytes(const rans_blocks *a, const rans_blocks *b, uint32_t units) {
+  uint64_t need = 0;
+  for (uint64_t m : {a->rows < kMatmulSlice ? a->rows : kMatmulSlice, a->rows % kMatmulSlice})
+    for (uint64_t n : {b->rows < kMatmulSlice ? b->rows : kMatmulSlice, b->rows % kMatmulSlice}) {
+      const uint64_t bytes = matmul_part_bytes(matmul_parts(m, n, a->cols, units), m, n);
+      need = bytes > need ? bytes : need;
+    }
+  return align_up((size_t)need, 256);
+}
+inline uint32_t matmul_units() {
+  const uint32_t units = compute_units();
+  return units ? units : 256;
+}
 
 }  // namespace
 
@@ -373,7 +384,7 @@ int rans_matmul_workspace_bytes(const rans_blocks *a, const rans_blocks *b, size
   const int rc = check_matmul(a, b);
   if (rc) return rc;
   if (!ws_bytes) return RANS_ERR_ARG;
-  *ws_bytes = matmul_ws_bytes(a, b);
+  *ws_bytes = matmul_ws_bytes(a, b, matmul_units());
   return RANS_OK;
 }
 
@@ -393,7 +404,8 @@ int rans_block_matmul(const uint8_t *d_a, const void *d_a_scale, const rans_bloc
   hipStream_t st = (hipStream_t)stream;
   const StreamDevice on(st);
   if (!on.ok) return RANS_ERR_HIP;
-  const size_t need = matmul_ws_bytes(a, b);
+  const uint32_t units = matmul_units();
+  const size_t need = matmul_ws_bytes(a, b, units);
   if (need && (!d_ws || !aligned_to(d_ws, 256))) return RANS_ERR_ARG;
   if (ws_bytes < need) return RANS_ERR_WORKSPACE;
   const int fmt = (a->format == RANS_E5M2 ? 2 : 0) + (b->format == RANS_E5M2 ? 1 : 0);
@@ -408,7 +420,8 @@ int rans_block_matmul(const uint8_t *d_a, const void *d_a_scale, const rans_bloc
       p.c = (uint8_t *)d_c + (m * ld_c + n) * eb, p.ldc = ld_c;
       p.m = (uint32_t)nm, p.n = (uint32_t)nn, p.k = (uint32_t)a->cols;
       p.e8m0 = a->scale_type == RANS_SCALE_E8M0, p.b_tile = b->block == RANS_BLOCK_TILE, p.out = out_dtype;
-      rc = out_dtype == RANS_F32 ? launch_matmul_wide(p, fmt, d_ws, st) : launch_matmul_narrow(p, fmt, d_ws, st);
+      const MatmulParts parts = matmul_parts(nm, nn, a->cols, units);
+      rc = out_dtype == RANS_F32 ? launch_matmul_wide(p, fmt, parts, d_ws, st) : launch_matmul_narrow(p, fmt, parts, d_ws, st);
       if (rc) return rc;
     }
   return RANS_OK;

@@ -17,11 +17,10 @@
 // Tiles by the least estimate.  B in E5M2, which no path of a training step has, takes the 128 x 128 tiles at every size.  The
 // large tiles are not for binary32 scales of both operands' rows, which leave them too few registers (4096 x 4096 x 11231: 574
 // us, 128 x 128 tiles 347).
-int launch_matmul_narrow(const MatmulArgs &p, int fmt, void *ws, hipStream_t st) {
+int launch_matmul_narrow(const MatmulArgs &p, int fmt, MatmulParts parts, void *ws, hipStream_t st) {
   const uint32_t units = compute_units() ? compute_units() : 256;
   const double large = mm_cost_large(p, units), medium = mm_cost_medium(p, units), small = mm_cost_small(p, units);
   const bool few = mm_few(p, small), fetch = mm_fetch_fits(p), deep = mm_deep(p, units, 8);
-  const MatmulParts parts = matmul_parts(p.m, p.n, p.k);
   return by_format(fmt, [&](auto fa, auto fb) {
     return by_scale(p, [&](auto scale) {
       constexpr int FA = decltype(fa)::value, FB = decltype(fb)::value, SCALE = decltype(scale)::value;
@@ -40,8 +39,7 @@ int launch_matmul_narrow(const MatmulArgs &p, int fmt, void *ws, hipStream_t st)
   });
 }
 
-MatmulParts matmul_parts(uint64_t m, uint64_t n, uint64_t k) {
-  const uint32_t units = compute_units() ? compute_units() : 256;
+MatmulParts matmul_parts(uint64_t m, uint64_t n, uint64_t k, uint32_t units) {
   const uint64_t tiles = (m + MmSmall::bm - 1) / MmSmall::bm * ((n + MmSmall::bn - 1) / MmSmall::bn), nb = (k + kBlk - 1) / kBlk;
   if (!tiles || 2 * tiles > units || nb < 32) return MatmulParts{1, 0};
   MatmulArgs p = {};

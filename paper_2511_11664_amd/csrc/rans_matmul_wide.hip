@@ -14,11 +14,10 @@
 #include "rans_matmul.h"
 #include "rans_matmul_pick.h"
 
-int launch_matmul_wide(const MatmulArgs &p, int fmt, void *ws, hipStream_t st) {
+int launch_matmul_wide(const MatmulArgs &p, int fmt, MatmulParts parts, void *ws, hipStream_t st) {
   const uint32_t units = compute_units() ? compute_units() : 256;
   const double medium = mm_cost_medium(p, units), small = mm_cost_small(p, units);
   const bool few = mm_few(p, small), fetch = mm_fetch_fits(p), deep = mm_deep(p, units, 1);
-  const MatmulParts parts = matmul_parts(p.m, p.n, p.k);
   return by_format(fmt, [&](auto fa, auto fb) {
     return by_scale(p, [&](auto scale) {
       constexpr int FA = decltype(fa)::value, FB = decltype(fb)::value, SCALE = decltype(scale)::value;

@@ -218,3 +218,22 @@ def test_memory_of_a_workspace():
     assert B._mem_ws(torch.empty(1, dtype=torch.uint8).expand(4096), -1)[1] == 1 and B._mem_ws(whole[:, :128], -1) == (at, (4 * 256 + 128) * 4)
     with pytest.raises(B._Refused):
         B._mem_ws(whole, 0)
+
+
+@pytest.mark.parametrize("k", (4096, 8192, 16384))
+@pytest.mark.parametrize("other", (1, 33, 64, 200, 2048, 4096))
+@pytest.mark.parametrize("left", (0, 1, 64, 77, 1024, 4000))
+def test_matmul_workspace_holds_every_launch(lib, left, other, k):
+    """A product of more than 2^17 rows goes launch by launch: what the whole asks for is enough for the launch of the rows that
+    are left, which alone may have few enough tiles to take K in parts."""
+    slice_rows = 1 << 17
+
+    def need(m, n):
+        size = C.c_size_t()
+        assert lib.rans_matmul_workspace_bytes(B.make_blocks(m, k), B.make_blocks(n, k), C.byref(size)) == B.OK
+        return size.value
+
+    for whole in (slice_rows + left, 3 * slice_rows + left):
+        assert need(whole, other) >= max(need(left, other), need(slice_rows, other))
+        assert need(other, whole) >= max(need(other, left), need(other, slice_rows))
+        assert need(whole, whole) >= need(left, left)

@@ -282,3 +282,28 @@ def test_launched_kernels(launched_kernels):
         a, b = (coded(r, k, 0, False, False, r, tight=bool(kw)) for r in (m, n))
         for out in (torch.bfloat16, torch.float32):
             assert launched_kernels(lambda: product(a, b, out)) == names, (m, n, k)
+
+
+@pytest.mark.parametrize("long_a", (False, True))
+@pytest.mark.parametrize("out", (torch.float32, torch.bfloat16))
+def test_matmul_in_parts_behind_a_whole_launch(out, long_a, launched_kernels):
+    """More rows than a launch, and so few behind them that their launch alone takes K in parts: 2^17 rows, the same 1024 over and
+    over, and 77 others."""
+    k, few, again = 4096, 64, 128
+    x, y, rest = coded(few, k, 0, False, False, 1), coded(1024, k, 0, False, False, 2), coded(77, k, 0, False, False, 3)
+    code, scale = (torch.cat([y[i].repeat(again, 1), rest[i]]) for i in (0, 1))
+    long = (code, scale, B.make_blocks(1024 * again + 77, k, k, k // 128))
+    a, b = (long, x) if long_a else (x, long)
+    m, n = a[2].rows, b[2].rows
+    size = B.rans_matmul_workspace_bytes(a[2], b[2])[1]
+    assert size >= 2 * few * 77 * 4
+    ws, c = B.workspace(size), torch.full((m, n), 99.0, dtype=out, device="cuda")
+    assert B.rans_block_matmul(*a[:3], *b[:3], OUT[out], c, n, None) == B.ERR_ARG
+    assert B.rans_block_matmul(*a[:3], *b[:3], OUT[out], c, n, ws[:size - 256]) == B.ERR_WORKSPACE
+    torch.cuda.synchronize()
+    assert (c == 99).all()
+    assert "k_block_matmul_sum" in launched_kernels(lambda: B.rans_block_matmul(*a[:3], *b[:3], OUT[out], c, n, ws))
+    rows = c if long_a else c.t()
+    assert torch.equal(rows[1024:1024 * again].reshape(again - 1, 1024, few), rows[:1024].expand(again - 1, 1024, few))
+    for got, part in ((rows[:1024], y), (rows[1024 * again:], rest)):
+        check(got if long_a else got.t(), part if long_a else x, x if long_a else part, out, (m, n))
