@@ -179,7 +179,8 @@ int check_norm(const rans_norm_params *p) {
   return RANS_OK;
 }
 
-constexpr uint32_t kNormSliceRows = 1u << 21;  // rows of a launch
+constexpr uint32_t kNormSliceRows = 1u << 21;  // rows of a launch, whose threads stay below 2^32
+constexpr uint64_t kNormSliceCols = 1u << 26;  // columns of a launch of the weight gradient's sum
 
 // The work-group that a row takes: f(threads, eights a thread); 0 eights: any length.
 template <int NT, int NV, typename F> int with_row(F f) { return f(std::integral_constant<int, NT>{}, std::integral_constant<int, NV>{}); }
@@ -334,8 +335,9 @@ int rans_norm_backward(const void *d_dy, const void *d_dsum, const void *d_sum, 
     });
     if (rc) return rc;
   }
-  if (d_dweight && !both) {
-    PROF_LAUNCH(KID_NORM_DW, k_norm_dw, dim3((uint32_t)((p->cols + 31) / 32)), dim3(kDwWG), 0, st, (const float *)d_ws, g, (uint32_t)p->cols,
+  for (uint64_t c = 0; d_dweight && !both && c < p->cols; c += kNormSliceCols) {
+    const uint64_t n = p->cols - c < kNormSliceCols ? p->cols - c : kNormSliceCols;
+    PROF_LAUNCH(KID_NORM_DW, k_norm_dw, dim3((uint32_t)((n + 31) / 32)), dim3(kDwWG), 0, st, (const float *)d_ws, g, (uint32_t)c, (uint32_t)p->cols,
                 d_dweight);
     LAUNCH_CHECK();
   }

@@ -327,9 +327,9 @@ template <typename T, typename W, int NT, int NV> __global__ __launch_bounds__(N
 // dw[c] = sum of the partial rows, in a fixed order: 32 columns a work-group, every 32nd partial row a half wave, eight of
 // them requested at a time.  256 x 4096: 4.9 us, most of it launch and trips to memory.
 constexpr int kDwWG = 1024;
-__global__ __launch_bounds__(kDwWG) void k_norm_dw(const float *__restrict__ part, uint32_t n_part, uint32_t cols, float *__restrict__ dw) {
+__global__ __launch_bounds__(kDwWG) void k_norm_dw(const float *__restrict__ part, uint32_t n_part, uint32_t col0, uint32_t cols, float *__restrict__ dw) {
   __shared__ float s[kDwWG];
-  const uint32_t t = threadIdx.x, c = blockIdx.x * 32 + (t & 31), first = t >> 5;
+  const uint32_t t = threadIdx.x, c = col0 + blockIdx.x * 32 + (t & 31), first = t >> 5;
   constexpr uint32_t step = kDwWG / 32;
   float v = 0;
   if (c < cols) {

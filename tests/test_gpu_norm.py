@@ -305,3 +305,19 @@ def test_norm_codes_are_the_definitions():
     # a code is wrong where a multiple of half a step lies within y's error, some 2^-23 of y: of 2^21 codes about 2^21 2^-23 2^4 2 = 8
     assert off.sum() <= 40
     assert ((got - v).abs() <= step / 2 + 2.0 ** -22 * v.abs()).all()
+
+
+def test_norm_backward_of_more_columns_than_a_grid_has_threads():
+    """32 threads a column are 2^32 of them for 2^27 columns, more than a launch holds: several launches."""
+    cols = (1 << 27) + 300
+    g = torch.Generator(device="cuda").manual_seed(1)
+    dy, h = (torch.randn(1, cols, generator=g, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    rstd = torch.full((1,), 0.75, device="cuda")
+    p = params(1, cols, torch.bfloat16, torch.bfloat16)
+    dx, dw = torch.empty_like(h), torch.full((cols,), 3.0, device="cuda")
+    assert B.rans_norm_backward(dy, None, h, None, rstd, p, dx, dw, B.workspace(B.rans_norm_workspace_bytes(p)[1])) == 0
+    # one row: a product of three factors of which the first two have few bits, rounded once or twice; then a sum of one
+    for at in range(0, cols, 1 << 24):
+        part = slice(at, at + (1 << 24))
+        want = dy[0, part].double() * h[0, part].double() * 0.75
+        assert ((dw[part].double() - want).abs() <= 2 * U * want.abs()).all(), at
