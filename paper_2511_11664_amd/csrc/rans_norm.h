@@ -6,9 +6,9 @@
 // addition and the backward pass read;  rstd = 1 / sqrt(sum h^2 / K + eps);  y = h * rstd * w, half a step of binary32 off
 // and a little (rstd is kept in two parts);  codes and scales of y by the row blocks of rans_blocks.h, and / or y itself.
 // Backward:  g = dy * w, xh = h * rstd;  dx = rstd * (g - xh * sum(g * xh) / K) + dsum;  dw = sum over rows of dy * xh.
-// Sums of a row's squares: eight neighbours in binary32, whose errors average out, the rest in binary64, which costs two
-// instructions for eight elements.  The backward's sums are binary32: a lane's own eight neighbours (and every further eight),
-// then the lanes of a wave, then the waves.
+// Squares of a row and their sum are binary64: no finite h overflows or vanishes there, and the sum's error does not show in
+// rstd.  The backward's sums are binary32: a lane's own eight neighbours (and every further eight), then the lanes of a wave,
+// then the waves.
 //
 // Bound by memory: each tensor is read once and written once, a row lives in registers between its sum and its output.
 #pragma once
@@ -43,17 +43,29 @@ struct NormFwd {
 // 1 / sqrt(sum / cols + eps) as the nearest binary32 number and what it leaves: the approximate reciprocal root r of the mean m,
 // whose own rounding errors are kept beside it, takes one step r + r / 2 (1 - m r^2).  Codes are a rounding of y to a few bits,
 // and y is off by half a step of binary32 and not by one or two, so that fewer of them fall on the other side of a tie.
+// Rows far from one, whose reciprocal root may pass binary32's range: h is multiplied by `pre`, a power of two, and r + low is
+// the reciprocal root over it.  `out`: what the backward pass gets.
 struct Rstd {
-  float r, low;
+  float r, low, pre, out;
 };
 __device__ __forceinline__ Rstd rstd_of(double sum, const NormFwd &a) {
   const double mean = sum * a.inv_cols + (double)a.eps;
   const float m = (float)mean, m_low = (float)(mean - (double)m);
-  if (!(m >= 0x1p-100f && m < 0x1p100f)) return Rstd{1.0f / sqrtf(m), 0.0f};
+  if (!(m >= 0x1p-100f && m < 0x1p100f)) {
+    if (!(mean > 0 && mean < (double)INFINITY)) {
+      const float r = 1.0f / sqrtf(m);
+      return Rstd{r, 0.0f, 1.0f, r};
+    }
+    // least mean 2^-328 (one subnormal number in 2^30): h * 2^64 is below 2^14 sqrt(K); largest 2^256
+    const float pre = mean < 1 ? 0x1p64f : 0x1p-32f;
+    const double d = 1.0 / sqrt(mean), q = d / (double)pre;
+    const float r = (float)q;
+    return Rstd{r, (float)(q - (double)r), pre, (float)d};
+  }
   const float r = __builtin_amdgcn_rsqf(m), t = m * r, t_low = __builtin_fmaf(m_low, r, __builtin_fmaf(m, r, -t));
   const float step = 0.5f * r * __builtin_fmaf(-t_low, r, __builtin_fmaf(-t, r, 1.0f));
   const float high = r + step;
-  return Rstd{high, (r - high) + step};
+  return Rstd{high, (r - high) + step, 1.0f, high};
 }
 
 // A row per work-group of NT threads, NV times eight neighbouring elements a thread (NV = 0: any length, h read again).
@@ -69,7 +81,7 @@ __global__ __launch_bounds__(NT) void k_norm_quant(NormFwd a, uint64_t row0) {
   const T *res = a.res ? (const T *)a.res + row * a.ld_res : nullptr;
   T *sum = a.sum ? (T *)a.sum + row * a.ld_sum : nullptr;
   double acc = 0;
-  Rstd rstd = {0, 0};
+  Rstd rstd = {0, 0, 1, 0};
   auto add = [&](V v, V r) {
     f32x8 h = float8_of(v);
     if (res) {
@@ -79,14 +91,18 @@ __global__ __launch_bounds__(NT) void k_norm_quant(NormFwd a, uint64_t row0) {
     return h;
   };
   auto square = [&](f32x8 h) {
-    float q[4];
+    double q[2] = {0, 0};  // two chains: a link waits for the one before
 #pragma unroll
-    for (int i = 0; i < 4; i++) q[i] = __builtin_fmaf(h[i], h[i], h[i + 4] * h[i + 4]);
-    acc += (double)((q[0] + q[1]) + (q[2] + q[3]));
+    for (int i = 0; i < 8; i++) q[i & 1] = __builtin_fma((double)h[i], (double)h[i], q[i & 1]);
+    acc += q[0] + q[1];
   };
   auto weight8 = [&](uint32_t c) { return a.weight ? load8((const W *)a.weight, c, n) : (f32x8){1, 1, 1, 1, 1, 1, 1, 1}; };
   auto give = [&](uint32_t c, f32x8 h8, f32x8 w) {
     // 16 lanes hold a block; lanes behind the row's end hold zeros and take part in its maximum
+    if (rstd.pre != 1) {
+#pragma unroll
+      for (int i = 0; i < 8; i++) h8[i] *= rstd.pre;
+    }
     // h * rstd in two parts times w; an infinite w meets the lower part as a finite one
     auto lower = [&](int i, float x) { return __builtin_fmaf(h8[i], rstd.low, __builtin_fmaf(h8[i], rstd.r, -x)) * __builtin_amdgcn_fmed3f(w[i], -0x1.fffffep127f, 0x1.fffffep127f); };
     f32x8 v;
@@ -161,7 +177,7 @@ __global__ __launch_bounds__(NT) void k_norm_quant(NormFwd a, uint64_t row0) {
       give(c, h, weight8(c));
     }
   }
-  if (a.rstd && t == 0) a.rstd[row] = rstd.r;
+  if (a.rstd && t == 0) a.rstd[row] = rstd.out;
 }
 
 struct NormBwd {

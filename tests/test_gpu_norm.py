@@ -321,3 +321,25 @@ def test_norm_backward_of_more_columns_than_a_grid_has_threads():
         part = slice(at, at + (1 << 24))
         want = dy[0, part].double() * h[0, part].double() * 0.75
         assert ((dw[part].double() - want).abs() <= 2 * U * want.abs()).all(), at
+
+
+@pytest.mark.parametrize("dtype, size", [(torch.float32, s) for s in (1e36, 1e25, 1e18, 1e-18, 1e-25, 1e-36, 1e-40)] + [(torch.bfloat16, 1e30), (torch.bfloat16, 1e-30)])
+def test_norm_of_rows_whose_squares_pass_binary32(dtype, size):
+    """Squares are binary64: no finite row becomes zeros or infinities.  rstd is one rounding to binary32 off, of half a step of its
+    subnormal numbers at least (and an infinity behind the largest); y as everywhere."""
+    for rows, cols in ((3, 1000), (2, 8200)):
+        x, r, w = data(rows, cols, torch.float32)
+        x, r = (x * size).to(dtype), (r * size).to(dtype)
+        h, rstd, y = O.norm(x, r, w, 0.0, dtype)
+        assert (h == h).all() and torch.isfinite(h).all()
+        p = B.make_norm_params(rows, cols, CODE[dtype], B.F32, 0.0)
+        got_rstd, out, m = torch.zeros(rows, device="cuda"), torch.empty(rows, cols, dtype=dtype, device="cuda"), B.BlockMatrix(rows, cols)
+        assert B.rans_norm_quantize(x.cuda(), r.cuda(), w.cuda(), p, None, got_rstd, out, m.code, m.scale, m.layout) == 0
+        for row in range(rows):
+            if (h[row] == 0).all():
+                continue
+            got, want = got_rstd[row].item(), rstd[row].item()
+            assert abs(got - want) <= rstd_tolerance(cols) * want + 2.0 ** -150 if want < 3.4e38 else got == float("inf")
+            assert ((out[row].cpu().double() - y[row]).abs() <= (rstd_tolerance(cols) + 3 * U) * 1.01 * y[row].abs() + half_step(y[row], dtype)).all()
+            check_codes(y[row:row + 1], torch.full((1, 1), rstd_tolerance(cols) + 3 * U, dtype=torch.float64), m.code[row:row + 1, :cols],
+                        m.scale[row:row + 1, :-(-cols // 128)], 0, False)
