@@ -240,10 +240,13 @@ int rans_block_dequantize(const uint8_t *d_code, const void *d_scale, const rans
 /* The residual's addition and the root-mean-square norm in front of a layer, its output coded:
  *   h = x + residual rounded to dtype, rstd = 1 / sqrt(mean(h^2) + eps), y = h * rstd * weight (binary32),
  * each row by itself, whatever its magnitude: squares and their sum are binary64, y needs no rstd in binary32's range.  The
- * rstd that is stored is binary32: below 2^-126 it has fewer bits, above 2^128 (eps = 0) it is an infinity.  x, residual, sum, y: rows x cols elements of dtype, ld_* elements from a row to the next; weight:
- * cols elements of dtype or binary32.  d_res, d_weight (all ones) and each of the outputs d_sum (h), d_rstd (binary32, one
- * a row, for rans_norm_backward), d_y (y rounded to dtype) and d_code / d_scale (y coded as `out` says, RANS_BLOCK_ROW)
- * may be NULL.  d_sum and d_y may be d_x's or d_res's own memory (same pointer, same ld).  Every ld_* is at least cols. */
+ * rstd that is stored is binary32: below 2^-126 it has fewer bits, above 2^128 (eps = 0) it is an infinity.
+ * x, residual, sum, y: rows x cols elements of dtype, ld_* elements from a row to the next; weight: cols elements of dtype or
+ * binary32.  d_res, d_weight (all ones) and each of the outputs d_sum (h), d_rstd (binary32, one a row, for
+ * rans_norm_backward), d_y (y rounded to dtype) and d_code / d_scale (y coded as `out` says, RANS_BLOCK_ROW) may be NULL.
+ * Codes under binary32 scales are those of binary32's y.  Under powers of two, which are exact, they are those of y before that
+ * rounding: a y that binary32 puts on a border between two codes or two scales is coded by the side on which it lies, where
+ * rans_block_quantize of a binary32 d_y takes the even code or the smaller scale.  d_sum and d_y may be d_x's or d_res's own memory (same pointer, same ld).  Every ld_* is at least cols. */
 typedef struct {
   uint64_t rows, cols;  /* cols >= 1 */
   uint64_t ld_x, ld_res, ld_sum, ld_y;

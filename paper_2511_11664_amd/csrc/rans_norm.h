@@ -106,28 +106,31 @@ __global__ __launch_bounds__(NT) void k_norm_quant(NormFwd a, uint64_t row0) {
     // h * rstd in two parts times w; an infinite w meets the lower part as a finite one
     auto lower = [&](int i, float x) { return __builtin_fmaf(h8[i], rstd.low, __builtin_fmaf(h8[i], rstd.r, -x)) * __builtin_amdgcn_fmed3f(w[i], -0x1.fffffep127f, 0x1.fffffep127f); };
     f32x8 v;
-    uint32_t tie = 1;  // 0 where a y lies halfway between two codes, as far as its binary32 tells
+    // 0 where a y may lie on a border under powers of two, as far as its binary32 tells: halfway between two codes (normal ones
+    // have one bit more than a code there, subnormal ones fewer) or at a scale's largest number
+    uint32_t border = 1;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
       const float x = h8[i] * rstd.r;
       v[i] = __builtin_fmaf(x, w[i], lower(i, x));
       if (E8M0) {
-        const uint32_t t = (__float_as_uint(v[i]) << (a.e5m2 ? 11 : 12)) + 0x80000000u;
-        tie = t < tie ? t : tie;
+        const uint32_t low = __float_as_uint(v[i]) << (a.e5m2 ? 12 : 13);
+        border = low < border ? low : border;
       }
     }
     if (a.y && c < n) store8((T *)a.y + row * a.ld_y, c, n, v);
     if (a.codes) {
-      const BlockScale s = block_scale<E8M0>(max16(abs_max8(v)), a.e5m2);
-      if (E8M0 && tie == 0) {
-        // powers of two leave a y where it is between two codes: what binary32 dropped decides
+      if (E8M0 && border == 0 && c < n) {
+        // powers of two leave a y on its side of a border: what binary32 dropped decides, as the next number on that side (a y
+        // below some 2^-120 may have dropped what no binary32 number holds, and stays)
 #pragma unroll
         for (int i = 0; i < 8; i++) {
           const uint32_t b = __float_as_uint(v[i]);
           const float x = h8[i] * rstd.r, rest = __builtin_fmaf(x, w[i], -v[i]) + lower(i, x);
-          if ((b << (a.e5m2 ? 11 : 12)) == 0x80000000u && rest != 0) v[i] = __uint_as_float((rest > 0) == (v[i] > 0) ? b + 1 : b - 1);
+          if (b << (a.e5m2 ? 12 : 13) == 0 && v[i] != 0 && (rest > 0 || rest < 0)) v[i] = __uint_as_float((rest > 0) == (v[i] > 0) ? b + 1 : b - 1);
         }
       }
+      const BlockScale s = block_scale<E8M0>(max16(abs_max8(v)), a.e5m2);
       if (c < n) {
         store_codes8(a.codes + row * a.ld, c, n, codes8(v, s.factor, a.e5m2));
         if ((t & 15) == 0) store_scale<E8M0>(a.scales, row * a.ld_scale + c / kBlk, s);

@@ -343,3 +343,68 @@ def test_norm_of_rows_whose_squares_pass_binary32(dtype, size):
             assert ((out[row].cpu().double() - y[row]).abs() <= (rstd_tolerance(cols) + 3 * U) * 1.01 * y[row].abs() + half_step(y[row], dtype)).all()
             check_codes(y[row:row + 1], torch.full((1, 1), rstd_tolerance(cols) + 3 * U, dtype=torch.float64), m.code[row:row + 1, :cols],
                         m.scale[row:row + 1, :-(-cols // 128)], 0, False)
+
+
+def norm_codes(x, w, fmt, e8m0):
+    """Codes, scales (their values) and rstd of a CPU matrix's norm, on the CPU."""
+    rows, cols = x.shape
+    m, rstd = B.BlockMatrix(rows, cols, fmt, int(e8m0)), torch.empty(rows, device="cuda")
+    assert B.rans_norm_quantize(x.cuda(), None, w.cuda(), params(rows, cols, x.dtype, w.dtype), None, rstd, None, m.code, m.scale, m.layout) == 0
+    s = m.scale[:, :-(-cols // 128)].cpu()
+    return O.decode8(m.code[:, :cols].cpu(), fmt), torch.exp2(s.double() - 127) if e8m0 else s.double(), rstd.cpu().double()
+
+
+@pytest.mark.parametrize("cols", (300, 4000, 9000))
+@pytest.mark.parametrize("fmt", (0, 1))
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+def test_norm_codes_on_borders_under_powers_of_two(dtype, fmt, cols):
+    """Weights that put y next to a border, less than half a step of binary32 from it: halfway between two codes, normal ones and
+    subnormal ones, or at the largest number of a scale.  A code and a scale go by the side on which y lies."""
+    g = torch.Generator().manual_seed(cols + fmt)
+    mbits, least = ((3, -6), (2, -14))[fmt]
+    x = torch.randn(1, cols, generator=g).to(dtype)
+    x[x.abs() < 0.01] = 0.01
+    odd = 2 * torch.randint(0, 1 << mbits, (cols,), generator=g) + 1
+    normal = (1 + odd.double() / (2 << mbits)) * torch.exp2(torch.randint(least, 6, (cols,), generator=g).double())
+    z = torch.where(torch.rand(cols, generator=g) < 0.5, normal, odd * 2.0 ** (least - mbits - 1))
+    block = torch.arange(cols) // 128
+    z[::128] = torch.where(block[::128] % 3 > 0, O.VMAX[fmt], 0.9 * O.VMAX[fmt]).double()
+    target = z * torch.exp2((block % 11 - 5).double())
+    rstd = O.norm(x, None, None, EPS, dtype)[1]
+    w = (target / (x[0].double() * rstd)).float()
+    y = O.norm(x, None, w, EPS, dtype)[2]
+    assert (y[0].float().double() == target).sum() > cols / 3 and (y[0] != target).all()  # binary32 alone does not see the side
+    s = O.block_scales(y, fmt, True, False)
+    got, got_s, _ = norm_codes(x, w, fmt, True)
+    assert torch.equal(got_s, s)
+    assert torch.equal(got, O.round8(y / O.spread(s, 1, cols, False), fmt))
+
+
+@pytest.mark.parametrize("rows, cols", ((512, 4096), (5000, 1000), (40, 8200), (300, 96)))
+@pytest.mark.parametrize("fmt", (0, 1))
+@pytest.mark.parametrize("dtype", tuple(CODE))
+def test_norm_codes_under_powers_of_two_are_exactly_the_definitions(dtype, fmt, rows, cols):
+    """y is known to some 2^-43 (eps is a binary32 number): of 2^21 codes, with 2^5 borders an octave at most, 2^-17 lie within that
+    of a border.  rstd is the nearest binary32 number but for as rare ones: half a step, and 2^-30 of it on top."""
+    x, _, w = data(rows, cols, dtype)
+    w = w.to(dtype)
+    _, rstd, y = O.norm(x, None, w, EPS, dtype)
+    s = O.block_scales(y, fmt, True, False)
+    got, got_s, got_rstd = norm_codes(x, w, fmt, True)
+    assert torch.equal(got_s, s)
+    assert torch.equal(got, O.round8(y / O.spread(s, rows, cols, False), fmt))
+    assert ((got_rstd - rstd).abs() <= U * (1 + 2.0 ** -6) * rstd).all()
+
+
+@pytest.mark.parametrize("fmt", (0, 1))
+def test_norm_codes_under_binary32_scales_are_those_of_y(fmt):
+    """The definition of the codes starts from binary32's y: what rans_block_quantize gives for it."""
+    for rows, cols in ((200, 4096), (3, 8200), (64, 333)):
+        x, r, w = data(rows, cols, torch.float32)
+        out, m, q = torch.empty(rows, cols, device="cuda"), B.BlockMatrix(rows, cols, fmt), B.BlockMatrix(rows, cols, fmt)
+        assert B.rans_norm_quantize(x.cuda(), r.cuda(), w.cuda(), params(rows, cols, torch.float32, torch.float32), None, None, out, m.code, m.scale, m.layout) == 0
+        q.quantize(out)
+        nb = -(-cols // 128)
+        assert torch.equal(m.code[:, :cols], q.code[:, :cols]) and torch.equal(m.scale[:, :nb], q.scale[:, :nb])
+        y = O.norm(x, r, w, EPS, torch.float32)[2]
+        assert ((out.cpu().double() - y).abs() <= U * (1 + 2.0 ** -6) * y.abs()).all()  # a rounding, and 2^-30 on top
