@@ -446,30 +446,41 @@ class BlockMatrix:
 
     def quantize(self, x: torch.Tensor, transpose=False):
         """Codes of a tensor [rows, cols] ([cols, rows] with `transpose`) whose last dimension is contiguous."""
-        self._check(rans_block_quantize(x, _ld(x), _dtype_code(x), transpose, self.code, self.scale, self.layout))
+        rows, cols = self.layout.rows, self.layout.cols
+        ld = _ld(x, cols, rows) if transpose else _ld(x, rows, cols)
+        self._check(rans_block_quantize(x, ld, _dtype_code(x), transpose, self.code, self.scale, self.layout))
         return self
 
     def dequantize(self, out: torch.Tensor):
-        self._check(rans_block_dequantize(self.code, self.scale, self.layout, _dtype_code(out), out, _ld(out)))
+        """The values, into a tensor [rows, cols] whose last dimension is contiguous."""
+        ld = _ld(out, self.layout.rows, self.layout.cols)
+        self._check(rans_block_dequantize(self.code, self.scale, self.layout, _dtype_code(out), out, ld))
         return out
 
     def matmul(self, b: "BlockMatrix", out: torch.Tensor, ws=None):
-        """out = self b^T; ws: rans_matmul_workspace_bytes() bytes, allocated where not given."""
+        """out [rows, b's rows] = self b^T; ws: rans_matmul_workspace_bytes() bytes, allocated where not given."""
+        ld, dtype = _ld(out, self.layout.rows, b.layout.rows), _dtype_code(out)
         if ws is None:
             rc, size = rans_matmul_workspace_bytes(self.layout, b.layout)
             self._check(rc)
             ws = workspace(size, out.device) if size else None
-        self._check(rans_block_matmul(self.code, self.scale, self.layout, b.code, b.scale, b.layout, _dtype_code(out), out, _ld(out), ws))
+        self._check(rans_block_matmul(self.code, self.scale, self.layout, b.code, b.scale, b.layout, dtype, out, ld, ws))
         return out
 
 
+_DTYPE_CODES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+
+
 def _dtype_code(t):
-    return {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}[t.dtype]
+    code = _DTYPE_CODES.get(t.dtype)
+    if code is None:
+        raise RansError(ERR_ARG)
+    return code
 
 
-def _ld(t):
-    """Elements from a row of a matrix to the next; its rows are contiguous."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+def _ld(t, rows=None, cols=None):
+    """Elements from a row of a matrix to the next; its rows are contiguous, and it is rows x cols where these are told."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (rows is not None and tuple(t.shape) != (rows, cols)):
         raise RansError(ERR_SHAPE)
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 

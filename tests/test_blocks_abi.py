@@ -237,3 +237,30 @@ def test_matmul_workspace_holds_every_launch(lib, left, other, k):
         assert need(whole, other) >= max(need(left, other), need(slice_rows, other))
         assert need(other, whole) >= max(need(other, left), need(other, slice_rows))
         assert need(whole, whole) >= need(left, left)
+
+
+def refused(code, call):
+    with pytest.raises(B.RansError) as e:
+        call()
+    assert e.value.code == code
+
+
+def test_block_matrix_refuses_other_shapes_and_types(lib):
+    """Larger tensors too, of which only a corner would be coded or written; the right shape passes on to the memory's check, which
+    refuses the host's."""
+    m, w = B.BlockMatrix(4, 256, device="cpu"), B.BlockMatrix(6, 256, device="cpu")
+    for rows, cols in ((8, 512), (8, 256), (4, 512), (3, 256), (4, 255), (256, 4)):
+        refused(B.ERR_SHAPE, lambda: m.quantize(torch.zeros(rows, cols)))
+        refused(B.ERR_SHAPE, lambda: m.quantize(torch.zeros(cols, rows), transpose=True))
+        refused(B.ERR_SHAPE, lambda: m.dequantize(torch.zeros(rows, cols)))
+    for rows, cols in ((8, 6), (4, 8), (4, 5), (6, 4), (4, 256)):
+        refused(B.ERR_SHAPE, lambda: m.matmul(w, torch.zeros(rows, cols)))
+    refused(B.ERR_SHAPE, lambda: m.quantize(torch.zeros(8, 512)[:4, ::2]))
+    refused(B.ERR_SHAPE, lambda: m.quantize(torch.zeros(4 * 256)))
+    refused(B.ERR_ARG, lambda: m.quantize(torch.zeros(4, 256, dtype=torch.float64)))
+    refused(B.ERR_ARG, lambda: m.dequantize(torch.zeros(4, 256, dtype=torch.int16)))
+    refused(B.ERR_ARG, lambda: m.matmul(w, torch.zeros(4, 6, dtype=torch.float64)))
+    refused(B.ERR_ARG, lambda: m.quantize(torch.zeros(4, 256)))
+    refused(B.ERR_ARG, lambda: m.quantize(torch.zeros(256, 9)[:, :4], transpose=True))
+    refused(B.ERR_ARG, lambda: m.dequantize(torch.zeros(4, 256)))
+    refused(B.ERR_ARG, lambda: m.matmul(w, torch.zeros(4, 6)))
