@@ -309,12 +309,30 @@ class _Refused(Exception):
 
 def _mem(t, dev, rows, cols, ld, size):
     """Address of a tensor on device `dev` whose memory reaches to the end of rows x cols elements of `size` bytes that are ld
-    apart; None for an absent one."""
+    apart; None for an absent one.  A tensor that is not contiguous has at least cols neighbours in a row, of one dimension or
+    of several."""
     if t is None:
         return None
-    if t.get_device() != dev or (rows and cols and ((rows - 1) * ld + cols) * size > (t.nbytes if t.is_contiguous() else _reach(t))):
+    if t.get_device() != dev:
         raise _Refused
+    if rows and cols:
+        whole = t.is_contiguous()
+        if not whole and _neighbours(t) < cols:
+            raise _Refused
+        if ((rows - 1) * ld + cols) * size > (t.nbytes if whole else _reach(t)):
+            raise _Refused
     return t.data_ptr()
+
+
+def _neighbours(t):
+    """Elements of a tensor, from its first one on in its own order, that follow one another in memory."""
+    n = 1
+    for size, stride in zip(reversed(t.shape), reversed(t.stride())):
+        if size != 1:
+            if stride != n:
+                break
+            n *= size
+    return n
 
 
 def _reach(t):

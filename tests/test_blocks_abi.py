@@ -264,3 +264,23 @@ def test_block_matrix_refuses_other_shapes_and_types(lib):
     refused(B.ERR_ARG, lambda: m.quantize(torch.zeros(256, 9)[:, :4], transpose=True))
     refused(B.ERR_ARG, lambda: m.dequantize(torch.zeros(4, 256)))
     refused(B.ERR_ARG, lambda: m.matmul(w, torch.zeros(4, 6)))
+
+
+def test_binding_refuses_strided_rows():
+    """Elements of a row, of a weight, of rstd follow one another in memory: other strides are not what the entry points read."""
+    x = torch.zeros(8, 512)
+
+    def holds(t, *want):
+        try:
+            return B._mem(t, -1, *want) == t.data_ptr()
+        except B._Refused:
+            return False
+
+    assert holds(x[:, :256], 8, 256, 512, 4) and holds(x.view(-1)[3:], 1, 256, 256, 4) and holds(x[:, 5:6], 8, 1, 512, 4)
+    assert holds(x[0, :256].expand(1, 256), 1, 256, 256, 4) and holds(x[:, 0], 1, 1, 1, 4)
+    heads = torch.zeros(8, 6, 64)[:, :4]                # heads next to one another, others behind them in each row
+    assert holds(heads, 8, 256, 384, 4) and holds(heads[:, :, None], 8, 256, 384, 4) and not holds(heads, 8, 257, 384, 4)
+    assert not holds(x[:, ::2], 8, 256, 512, 4) and not holds(x.t(), 8, 512, 512, 4)
+    assert not holds(x.view(-1)[::2], 1, 256, 256, 4)   # every other number
+    assert not holds(x[0, :1].expand(256), 1, 256, 256, 4)
+    assert not holds(x[:, 0], 1, 8, 8, 4) and not holds(x[:, :1], 1, 8, 8, 4)  # a column as a weight
