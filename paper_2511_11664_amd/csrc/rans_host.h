@@ -25,7 +25,9 @@ enum KernelId {
   KID_CSR_EXPAND, KID_DEQUANT, KID_RS_MASK, KID_RS_COUNT, KID_RS_COST,
   KID_ENCODE_FEED, KID_DECODE_LEAN, KID_BLOCK_QUANT, KID_BLOCK_QUANT_TILE, KID_BLOCK_DEQUANT, KID_NORM_QUANT, KID_NORM_BWD,
   KID_NORM_DW, KID_BLOCK_MATMUL, KID_BLOCK_MATMUL_FEW, KID_BLOCK_MATMUL_ANY,
-  KID_BLOCK_MATMUL_SUM, KID_NORM_BWD_BOTH, KID_COUNT
+  KID_BLOCK_MATMUL_SUM, KID_NORM_BWD_BOTH,
+  KID_BLOCK_MATMUL_128, KID_BLOCK_MATMUL_DEEP, KID_BLOCK_MATMUL_256, KID_BLOCK_MATMUL_ANY_128,  // larger tiles than the name alone: 64 x 64
+  KID_COUNT
 };
 inline const char *const kKernelNames[KID_COUNT] = {
     "k_minmax", "k_qinfo", "k_quant_hist", "k_scan_u32", "k_csr_compact", "k_csr_rows",
@@ -33,7 +35,8 @@ inline const char *const kKernelNames[KID_COUNT] = {
     "k_csr_to_dense", "k_dequant", "k_rs_mask", "k_rs_count", "k_rs_cost",
     "k_encode_feed", "k_decode_lean", "k_block_quant", "k_block_quant_tile", "k_block_dequant", "k_norm_quant", "k_norm_bwd",
     "k_norm_dw", "k_block_matmul", "k_block_matmul_few", "k_block_matmul_any",
-    "k_block_matmul_sum", "k_norm_bwd_both"};
+    "k_block_matmul_sum", "k_norm_bwd_both",
+    "k_block_matmul_128", "k_block_matmul_deep", "k_block_matmul_256", "k_block_matmul_any_128"};
 
 struct ProfRecord {
   int kid;
@@ -42,7 +45,7 @@ struct ProfRecord {
 struct Profiler {
   uint64_t mask = 0;
   uint32_t every = 1;                 // bracket every n-th launch of an enabled kernel
-  uint32_t seen[32] = {0};            // launches seen per kernel id since the last enable
+  uint32_t seen[KID_COUNT] = {0};     // launches seen per kernel id since the last enable
   std::vector<ProfRecord> recs;   // records in use
   std::vector<ProfRecord> pool;   // event pairs ready for reuse
   std::mutex mu;

@@ -18,14 +18,17 @@ inline uint32_t mm_parts_of(const MatmulArgs &p) { return p.part_blocks ? ((p.k 
 
 template <typename TILE, int FA, int FB, int SCALE, bool EXACT> int launch_tiles(const MatmulArgs &p, hipStream_t st) {
   const uint32_t tiles_m = (p.m + TILE::bm - 1) / TILE::bm, tiles_n = (p.n + TILE::bn - 1) / TILE::bn;
-  PROF_LAUNCH(KID_BLOCK_MATMUL, (k_block_matmul<TILE, FA, FB, SCALE, EXACT>), dim3(tiles_m * tiles_n, mm_parts_of(p)), dim3(TILE::threads), 0, st, p, tiles_m,
+  constexpr int kid = std::is_same<TILE, MmSmall>::value ? KID_BLOCK_MATMUL : std::is_same<TILE, MmLarge>::value ? KID_BLOCK_MATMUL_256
+                      : std::is_same<TILE, MmDeep>::value ? KID_BLOCK_MATMUL_DEEP : KID_BLOCK_MATMUL_128;
+  PROF_LAUNCH(kid, (k_block_matmul<TILE, FA, FB, SCALE, EXACT>), dim3(tiles_m * tiles_n, mm_parts_of(p)), dim3(TILE::threads), 0, st, p, tiles_m,
               tiles_n);
   LAUNCH_CHECK();
   return RANS_OK;
 }
 template <typename TILE, int FA, int FB, int SCALE, bool EXACT> int launch_any(const MatmulArgs &p, hipStream_t st) {
   const uint32_t tiles_m = (p.m + TILE::bm - 1) / TILE::bm, tiles_n = (p.n + TILE::bn - 1) / TILE::bn;
-  PROF_LAUNCH(KID_BLOCK_MATMUL_ANY, (k_block_matmul_any<TILE, FA, FB, SCALE, EXACT>), dim3(tiles_m * tiles_n, mm_parts_of(p)), dim3(TILE::threads), 0, st, p, tiles_m,
+  constexpr int kid = std::is_same<TILE, MmSmall>::value ? KID_BLOCK_MATMUL_ANY : KID_BLOCK_MATMUL_ANY_128;
+  PROF_LAUNCH(kid, (k_block_matmul_any<TILE, FA, FB, SCALE, EXACT>), dim3(tiles_m * tiles_n, mm_parts_of(p)), dim3(TILE::threads), 0, st, p, tiles_m,
               tiles_n);
   LAUNCH_CHECK();
   return RANS_OK;
