@@ -185,10 +185,12 @@ constexpr uint64_t kNormSliceCols = 1u << 26;  // columns of a launch of the wei
 // The work-group that a row takes: f(threads, eights a thread); 0 eights: any length.
 template <int NT, int NV, typename F> int with_row(F f) { return f(std::integral_constant<int, NT>{}, std::integral_constant<int, NV>{}); }
 
-// Forward.  Few rows are quicker with more threads on each, many with more in flight for each thread: 4096 columns, 512 threads
-// over 256: 1 row 2.96 / 3.45 us, 512 rows 5.1 / 5.4, 16384 rows 84.7 / 83.4.
+// Forward.  Few rows are quicker with more threads on each, many with more in flight for each thread.  Twice the threads / two
+// vectors a thread, kernel us, bf16: 4096 columns 8 rows 4.4 / 4.8, 512 5.8 / 5.7, 1024 9.3 / 9.4, 2048 14.1 / 13.6, 4096 22.7 /
+// 21.7, 16384 77 / 73; 5120 columns 128 rows 5.0 / 5.3, 1024 12.5 / 11.3, 2048 19.6 / 17.8, 16384 126 / 103.  binary32, 4096 columns:
+// 512 rows 8.2 / 9.4, 2048 22.9 / 23.5, 16384 170 / 172; 2500 columns 1024 rows 11.0 / 11.6, 2048 19.0 / 17.9, 16384 137 / 122.
 template <typename F> int by_row_forward(const rans_norm_params &p, F f) {
-  const bool many = p.rows >= 4096;
+  const bool many = p.rows >= 2048;
   if (p.cols <= 64 * 8) return with_row<64, 1>(f);
   if (p.cols <= 256 * 8) return with_row<256, 1>(f);
   if (p.cols <= 512 * 8) return many ? with_row<256, 2>(f) : with_row<512, 1>(f);

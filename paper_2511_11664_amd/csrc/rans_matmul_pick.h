@@ -43,6 +43,9 @@ template <int MT, int W, int AHEAD, int FA, int FB, int SCALE, bool EXACT> int l
 // (K = 4096, 256 units; 48 to 1024 rows of A, 1024 to 12288 of B).  Widened operands and operands of any alignment take
 // longer, but change between 64 x 64 and 128 x 128 tiles at the same sizes.  K = 4096, 64 x 64 / larger, us: 395 x 4096
 // widened 27 / 43, any alignment 31 / 40, both 39 / 84; 2048 x 4096 103 / 76, 88 / 57, 116 / 88.
+// 128 x 128 / 256 x 256 tiles beyond those rows, us, binary32 scales (powers of two): K = 4096, 1024 x 12288 61 / 61 (59 / 56), 2048 x
+// 12288 115 / 122 (107 / 109), which the estimate has the other way round, 4096 x 4096 80 / 69 (74 / 61), 16384 x 12288 960 / 816
+// (901 / 740); K = 12288, 2048 x 4096 116 / 171 (107 / 151), 4096 x 4096 225 / 186 (208 / 163), 16384 x 4096 937 / 827 (887 / 728).
 inline double mm_cost(uint64_t tiles, uint32_t units, double alone, double both) {
   const uint64_t slots = both > 0 ? 2ull * units : units, whole = tiles / slots, rest = tiles % slots;
   const double full = both > 0 ? both : alone;

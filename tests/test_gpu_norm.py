@@ -408,3 +408,39 @@ def test_norm_codes_under_binary32_scales_are_those_of_y(fmt):
         assert torch.equal(m.code[:, :cols], q.code[:, :cols]) and torch.equal(m.scale[:, :nb], q.scale[:, :nb])
         y = O.norm(x, r, w, EPS, torch.float32)[2]
         assert ((out.cpu().double() - y).abs() <= U * (1 + 2.0 ** -6) * y.abs()).all()  # a rounding, and 2^-30 on top
+
+
+@pytest.mark.parametrize("fmt", (0, 1))
+@pytest.mark.parametrize("dtype", tuple(CODE))
+def test_norm_of_many_rows(dtype, fmt):
+    """The form for many rows, two vectors a thread and more in flight: whole rows and such that end inside a thread's second one;
+    tolerances as above, codes under powers of two exactly."""
+    for rows, cols, odd in ((2100, 2500, False), (2048, 4096, False), (2050, 5121, True), (2060, 8190, True)):
+        x, r, w = data(rows, cols, dtype)
+        w = w.to(dtype)
+        h, rstd, y = O.norm(x, r, w, EPS, dtype)
+        ld, off = (cols + 3, 1) if odd else (cols, 0)
+        total, out, m, got_rstd = pitched(torch.zeros_like(x), ld, off), pitched(torch.zeros_like(x), ld + 1, off), B.BlockMatrix(rows, cols, fmt, 1), torch.zeros(rows, device="cuda")
+        p = params(rows, cols, dtype, dtype, ld_x=ld, ld_res=ld + 2, ld_sum=ld, ld_y=ld + 1)
+        assert B.rans_norm_quantize(pitched(x, ld, off), pitched(r, ld + 2, off), w.cuda(), p, total, got_rstd, out, m.code, m.scale, m.layout) == 0
+        assert torch.equal(total.cpu().double(), h)
+        assert ((got_rstd.cpu().double() - rstd).abs() <= U * (1 + 2.0 ** -6) * rstd).all()
+        assert ((out.cpu().double() - y).abs() <= U * (1 + 2.0 ** -6) * y.abs() * 1.01 + half_step(y, dtype)).all()
+        s = O.block_scales(y, fmt, True, False)
+        assert torch.equal(torch.exp2(m.scale[:, :-(-cols // 128)].cpu().double() - 127), s)
+        assert torch.equal(O.decode8(m.code[:, :cols].cpu(), fmt), O.round8(y / O.spread(s, rows, cols, False), fmt))
+        f = B.BlockMatrix(rows, cols, fmt)
+        assert B.rans_norm_quantize(total, None, w.cuda(), params(rows, cols, dtype, dtype, ld_x=ld), None, None, None, f.code, f.scale, f.layout) == 0
+        check_codes(y, torch.full((rows, 1), 2 * U, dtype=torch.float64), f.code[:, :cols], f.scale[:, :-(-cols // 128)], fmt, False)
+
+
+@pytest.mark.parametrize("dtype", tuple(CODE))
+def test_norm_backward_of_several_rows_a_work_group(dtype, launched_kernels):
+    """Each width's work-groups, with three rows and more one after the other."""
+    for rows, cols in ((5000, 300), (2100, 1000), (1100, 4000), (1100, 5000), (1100, 6001), (1100, 8300)):
+        dy, ds, h, w, rstd = bwd_data(rows, cols, dtype, False)
+        p = params(rows, cols, dtype, w.dtype)
+        dx, dw, ws = torch.empty_like(h, device="cuda"), torch.empty(cols, device="cuda"), B.workspace(B.rans_norm_workspace_bytes(p)[1])
+        args = [t.cuda() for t in (dy, ds, h, w, rstd)]
+        assert launched_kernels(lambda: B.rans_norm_backward(*args, p, dx, dw, ws)) == {"k_norm_bwd", "k_norm_dw"}
+        check_backward(rows, cols, dtype, dy, ds, h, w, rstd, dx, dw)
