@@ -256,7 +256,8 @@ __global__ __launch_bounds__(kWG) void k_block_quant(const T *__restrict__ x, ui
 // whose blocks run down the columns of x.  Transposed codes go through LDS, where a lane's eight rows of a column are
 // one 8-byte chunk; the chunk's place in its row of 128 bytes is turned by the column's number / 8, so that the 16 lanes
 // of a row of x write 16 different places.  11231 x 4096 bf16, transposed: 28.9 us, 4.8 TB/s: rows of 128 bytes are what a tile
-// writes at a time, and a work-group reads, waits and writes once.
+// writes at a time, and a work-group reads, waits and writes once.  Tiles with one scale, 12288 x 4096 bf16: 27.9 us, 5.4 TB/s;
+// transposed 30.5, 4.9.
 template <typename T, bool E8M0, bool TRANS, bool TILE>
 __global__ __launch_bounds__(kWG) void k_block_quant_tile(const T *__restrict__ x, uint64_t ld_x, uint32_t x_rows, uint32_t x_cols,
                                                           uint8_t *__restrict__ codes, uint64_t ld, void *__restrict__ scales,

@@ -64,7 +64,7 @@ inline bool mm_deep(const MatmulArgs &p, uint32_t units, uint32_t least_blocks) 
 
 // Few rows of A: the kernel for them takes about 2.6 us and what B, and A once for every 16 rows of B, take at 7.9 MB a us;
 // `tiles` is what the tile kernel would take for a block.  1 / 16 / 32 rows, K = 4096, us, few rows over 64 x 64 tiles:
-// 4096 rows of B 4.4 / 6.5 / 9.4 over 12, 12288 rows of B 9.6 / 15.3 / 24.7 over 13.
+// 4096 rows of B 4.3 / 7.2 / 9.8 over 12, 12288 rows of B 9.6 / 15.3 / 24.7 over 13.
 inline bool mm_few(const MatmulArgs &p, double tiles) {
   if (p.m > 32) return false;
   const double bytes = (double)p.n * p.k * (1 + p.m / 16.0), nb = (p.k + kBlk - 1) / kBlk;
